@@ -64,7 +64,8 @@ enum {
   PQ_ERR_UNSUPPORTED = -5, /* valid request this build does not implement       */
   PQ_ERR_CUDA = -6,        /* a CUDA runtime / driver call failed               */
   PQ_ERR_TIMEOUT = -7,     /* a device-side bounded wait ran out                */
-  PQ_ERR_TOO_LARGE = -8    /* problem needs more scratch than a fixed-size buffer holds */
+  PQ_ERR_TOO_LARGE = -8,   /* problem needs more scratch than a fixed-size buffer holds */
+  PQ_ERR_INDEX = -9        /* pq_device_status only: an index in device memory was out of range */
 };
 
 enum {
@@ -358,6 +359,91 @@ typedef struct pq_bwd_view {
   float* dl;
 } pq_bwd_view;
 int pq_bwd_view_init(const pq_desc* d, void* ws, pq_bwd_view* out);
+
+/* ---------------------------------------------------------------------------
+ * Between the projections of a decoder: a paged key-value cache, attention of one new token per sequence over it, and the
+ * norms around a block.
+ * ---------------------------------------------------------------------------
+ * Key-value cache.  Keys and values of `heads` heads live in pages of page_size positions,
+ *     K, V [num_pages][heads][page_size][pitch],   pitch = pq_kv_pitch(format, head_dim): head_dim rounded up to 16 bytes,
+ * zero behind head_dim.  Sequence s keeps position p in page page_table[s][p / page_size]; entries that no call needs are not
+ * read, pages may be shared by sequences.  PQ_KV_BF16 keeps the values; PQ_KV_INT8 quantises each position and head by Eq. 7-9,
+ *     gamma = 2^7 / max(max|x|, 1e-5),   code = clamp(rint(x gamma), -128, 127),   which stands for code / gamma,
+ * with gamma in k_gamma, v_gamma [num_pages][heads][page_size] fp32 (NULL for PQ_KV_BF16); of a row that holds an infinity
+ * or a NaN every value reads back as NaN.
+ * head_dim a multiple of 4, 8 to 256; page_size a multiple of 16; every count at least 1.  The struct is a HOST value, read
+ * before a call returns; its pointers are device pointers, 16-byte aligned.
+ *
+ * Indices from device memory (seq, pos, lens, page_table) are checked by the kernels: what does not exist is neither read nor
+ * written, pq_device_status then reports PQ_ERR_INDEX, and the outputs that depend on it are undefined. */
+enum { PQ_KV_BF16 = 0, PQ_KV_INT8 = 1 };
+typedef struct pq_kv_cache {
+  uint32_t size, flags;       /* sizeof(pq_kv_cache); flags must be 0 */
+  int32_t format, heads, head_dim, page_size, num_pages;
+  int32_t num_seqs, max_pages; /* page_table [num_seqs][max_pages] */
+  int32_t reserved;            /* 0 */
+  void *K, *V;
+  float *k_gamma, *v_gamma;
+  const int32_t* page_table;
+} pq_kv_cache;
+int pq_kv_pitch(int format, int head_dim);   /* 0 for a format or head_dim that is not taken */
+
+/* Writes `tokens` tokens to the cache: token i becomes position pos[i] of sequence seq[i]; pos[i] < 0 is padding, nothing of
+ * that token is written.  Tokens of a call name different places (two that name the same one leave a mixture there).
+ *   K, V: rows of heads x head_dim bf16, k_stride / v_stride values from row to row (0 = dense; a multiple of 4);
+ *   cos, sin [rope_rows][head_dim / 2] fp32 or NULL: rotary embedding of keys and queries.  With i < head_dim / 2,
+ *     x_i' = bf16(x_i cos - x_{i + head_dim/2} sin),   x_{i + head_dim/2}' = bf16(x_{i + head_dim/2} cos + x_i sin),
+ *     row pos[i] of the tables; products and sum each rounded in fp32;
+ *   Q, Q_out: queries, rows of q_heads x head_dim, rotated from Q (q_stride) to Q_out (dense), which may be Q itself where that is dense;
+ *     both NULL and q_heads 0 without queries.  Without cos they are copied.
+ * tokens = 0 is a call that does nothing. */
+int pq_kv_append(const pq_kv_cache* c, int tokens, const int32_t* seq, const int32_t* pos, const uint16_t* K, int64_t k_stride,
+                 const uint16_t* V, int64_t v_stride, const float* cos, const float* sin, int rope_rows, const uint16_t* Q, int64_t q_stride,
+                 int q_heads, uint16_t* Q_out, void* stream);
+
+/* Reads `tokens` places of the cache: row i of K_out, V_out [tokens][heads][head_dim] bf16 is what position pos[i] of sequence
+ * seq[i] stands for, rounded once; rows with pos[i] < 0 are left as they are. */
+int pq_kv_read(const pq_kv_cache* c, int tokens, const int32_t* seq, const int32_t* pos, uint16_t* K_out, uint16_t* V_out, void* stream);
+
+/* Attention of one token per sequence of the page table over what that sequence keeps:
+ *     O[s,h] = sum_j w_j V_j / sum_j w_j,   w_j = exp(scale (Q[s,h] . K_j)),   j < lens[s],
+ * K_j, V_j of cache head h / (q_heads / heads).  Scores, weights and sums in fp32, one rounding to bf16.  A sequence of length 0
+ * (and a row without any weight) gives zeros; one of negative length is padding, its row is left as it is.
+ *   Q: rows of q_heads x head_dim bf16, q_stride values apart (0 = dense; a multiple of 4); q_heads a multiple of heads;
+ *   lens [num_seqs] int32, at most max_pages * page_size;  scale finite;
+ *   O [num_seqs][q_heads][head_dim] bf16;  lse [num_seqs][q_heads] fp32 = log sum_j w_j (-infinity for none), or NULL;
+ *   ws: pq_attn_workspace_bytes bytes of any content, for one call at a time.
+ * Results do not depend on scheduling, but on how the batch is cut into shares: the same sequence in another batch may
+ * differ in the last bit. */
+size_t pq_attn_workspace_bytes(const pq_kv_cache* c, int q_heads);
+int pq_attn_decode(const pq_kv_cache* c, int q_heads, const uint16_t* Q, int64_t q_stride, const int32_t* lens, float scale, uint16_t* O,
+                   float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* The norms before and after a block with its gate and residual scale (x: the stream in front of the block, y: its output):
+ *     u = rms(y) post_weight, or y without one;   s = res_scale x + gate u;   h = rms(s) pre_weight,
+ *     rms(z) = z / sqrt(mean z^2 + eps).
+ *   x, y, x_out = bf16(s), h [T,N] bf16; post_weight, pre_weight [N] bf16; gate fp32, one number or, with PQ_SCALE_VECTOR in
+ *   flags, [N].  Optional: post_weight, gate (1); pre_weight and h together; x_out where h is wanted alone; y, without post_weight and gate
+ *   (u = 0: the norm of the stream alone).  s and h are each rounded once, h from the unrounded s.  x_out may be x, h may be y.
+ * T >= 1, N a multiple of 8, 8 <= N <= 16384; eps > 0; res_scale finite. */
+typedef struct pq_norm_desc {
+  uint32_t size, flags;       /* sizeof(pq_norm_desc); PQ_SCALE_VECTOR */
+  int32_t T, N;
+  float eps, res_scale;
+} pq_norm_desc;
+int pq_block_norm_forward(const pq_norm_desc* d, const uint16_t* x, const uint16_t* y, const uint16_t* post_weight, const float* gate,
+                          const uint16_t* pre_weight, uint16_t* x_out, uint16_t* h, void* stream);
+
+/* Its backward from dx_out, dh [T,N] bf16, the gradients of s and h (either may be NULL, not both; dh and pre_weight come
+ * together), x_out as the forward left it (read when dh is given), y (read with post_weight or gate):
+ *   dx, dy [T,N] bf16; dpost, dpre [N] fp32; dgate fp32 like gate.  Every gradient is OVERWRITTEN; sums over tokens in a fixed order.
+ *   With post_weight: dy, dpost; with gate: dy, dgate; with dh: dpre (PQ_ERR_NULL otherwise).  With neither post_weight nor gate
+ *   dy may be NULL (dy = dx / res_scale).  dx may be dx_out or dh.
+ *   ws: pq_block_norm_workspace_bytes(d) bytes of any content. */
+size_t pq_block_norm_workspace_bytes(const pq_norm_desc* d);
+int pq_block_norm_backward(const pq_norm_desc* d, const uint16_t* dx_out, const uint16_t* dh, const uint16_t* x_out, const uint16_t* y,
+                           const uint16_t* post_weight, const float* gate, const uint16_t* pre_weight, uint16_t* dx, uint16_t* dy, float* dpost,
+                           float* dgate, float* dpre, void* ws, size_t ws_bytes, void* stream);
 
 /* Test hook for the tensor-core engine: D[M,N] = A . B^T-style contraction with
  * raw accumulators written out (int32 for mode 0, fp32 otherwise), so that the

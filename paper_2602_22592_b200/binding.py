@@ -17,6 +17,8 @@ LIB_PATH = os.path.join(_HERE, "libpquant.so")
 PQ_OK = 0
 PQ_ERR_NULL, PQ_ERR_SHAPE, PQ_ERR_ALIGN, PQ_ERR_WORKSPACE = -1, -2, -3, -4
 PQ_ERR_UNSUPPORTED, PQ_ERR_CUDA, PQ_ERR_TIMEOUT, PQ_ERR_TOO_LARGE = -5, -6, -7, -8
+PQ_ERR_INDEX = -9
+PQ_KV_BF16, PQ_KV_INT8 = 0, 1
 PQ_SCALE_VECTOR = 1
 PQ_DECODE_DUMP_ACC = 2
 PQ_FUSED_RMSNORM = 8
@@ -25,17 +27,26 @@ PQ_PHASE_PACK, PQ_PHASE_FWD, PQ_PHASE_BWD, PQ_PHASE_DECODE = 0, 1, 2, 3
 
 EXPORTS = ("pq_status_string", "pq_workspace_bytes", "pq_saved_bytes", "pq_saved_view_init",
            "pq_decode_view_init", "pq_bwd_view_init", "pq_decode_batch", "pq_decode_pack_bytes", "pq_pack_decode", "pq_decode_pack_hp8_bytes", "pq_pack_decode_hp8", "pq_pack_weights", "pq_pack_weights_static", "pq_pack_experts", "pq_linear_forward", "pq_linear_forward_hp8", "pq_linear_forward_rms", "pq_ffn_workspace_bytes", "pq_ffn_forward", "pq_ffn_view_init", "pq_linear_backward", "pq_debug_gemm", "pq_debug_gemm_tile",
-           "pq_device_status", "pq_kernel_launches", "pq_profile_events", "pq_set_option")
+           "pq_device_status", "pq_kernel_launches", "pq_profile_events", "pq_set_option", "pq_kv_pitch", "pq_kv_append", "pq_kv_read",
+           "pq_attn_workspace_bytes", "pq_attn_decode", "pq_block_norm_forward", "pq_block_norm_workspace_bytes", "pq_block_norm_backward")
 
 KERNEL_IDS = dict(pack_sums=0, binarize_pack=1, router=2, route_scan=3, act_quant=4, hp_up=5, fwd=6, scatter_rows=7,
                   scaled_sign=8, bwd_dw=12, sum_partials=16, sum_scalar=17, debug=18, decode_prep=19, decode_main=20,
-                  decode_pack=23, decode_stream=24)
+                  decode_pack=23, decode_stream=24, kv_append=25, kv_read=26, attn_decode=27, attn_join=28, norm_fwd=29,
+                  norm_bwd=30, norm_sums=31)
 
 
 class PqError(RuntimeError):
     def __init__(self, fn: str, status: int):
         self.status = status
         super().__init__(f"{fn} failed: {status} ({pq_status_string(status)})")
+
+
+class PqArgumentError(ValueError):
+    """A tensor that cannot be handed to the library: its type, shape, layout or device."""
+
+    def __init__(self, fn: str, why: str):
+        super().__init__(f"{fn}: {why}")
 
 
 class pq_desc(ctypes.Structure):
@@ -73,6 +84,17 @@ class pq_ffn_view(ctypes.Structure):
 
 class pq_bwd_view(ctypes.Structure):
     _fields_ = [("dl", ctypes.c_void_p)]
+
+
+class pq_kv_cache(ctypes.Structure):
+    _fields_ = [("size", ctypes.c_uint32), ("flags", ctypes.c_uint32)] + [(n, ctypes.c_int32) for n in (
+        "format", "heads", "head_dim", "page_size", "num_pages", "num_seqs", "max_pages", "reserved")] + [
+        (n, ctypes.c_void_p) for n in ("K", "V", "k_gamma", "v_gamma", "page_table")]
+
+
+class pq_norm_desc(ctypes.Structure):
+    _fields_ = [("size", ctypes.c_uint32), ("flags", ctypes.c_uint32), ("T", ctypes.c_int32), ("N", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("res_scale", ctypes.c_float)]
 
 
 _lib = None
@@ -130,6 +152,23 @@ def lib() -> ctypes.CDLL:
         L.pq_ffn_view_init.argtypes = [fp, vp, ctypes.POINTER(pq_ffn_view)]
         L.pq_linear_backward.restype = ci
         L.pq_linear_backward.argtypes = [dp] + [vp] * 9 + [vp, sz] + [vp] * 7 + [vp, sz, vp]
+        kp, i64, np_ = ctypes.POINTER(pq_kv_cache), ctypes.c_int64, ctypes.POINTER(pq_norm_desc)
+        L.pq_kv_pitch.restype = ci
+        L.pq_kv_pitch.argtypes = [ci, ci]
+        L.pq_kv_append.restype = ci
+        L.pq_kv_append.argtypes = [kp, ci, vp, vp, vp, i64, vp, i64, vp, vp, ci, vp, i64, ci, vp, vp]
+        L.pq_kv_read.restype = ci
+        L.pq_kv_read.argtypes = [kp, ci, vp, vp, vp, vp, vp]
+        L.pq_attn_workspace_bytes.restype = sz
+        L.pq_attn_workspace_bytes.argtypes = [kp, ci]
+        L.pq_attn_decode.restype = ci
+        L.pq_attn_decode.argtypes = [kp, ci, vp, i64, vp, ctypes.c_float, vp, vp, vp, sz, vp]
+        L.pq_block_norm_forward.restype = ci
+        L.pq_block_norm_forward.argtypes = [np_] + [vp] * 8
+        L.pq_block_norm_workspace_bytes.restype = sz
+        L.pq_block_norm_workspace_bytes.argtypes = [np_]
+        L.pq_block_norm_backward.restype = ci
+        L.pq_block_norm_backward.argtypes = [np_] + [vp] * 13 + [sz, vp]
         L.pq_debug_gemm.restype = ci
         L.pq_debug_gemm.argtypes = [ci, ci, ci, ci, vp, vp, vp, vp]
         L.pq_debug_gemm_tile.restype = ci
@@ -371,6 +410,151 @@ def pq_linear_backward(d, dY, X, w_s8, w_scales, A, B, Wr, alpha, beta, saved, d
         ctypes.byref(d), _ptr(dY), _ptr(X), _ptr(w_s8), _ptr(w_scales), _ptr(A), _ptr(B), _ptr(Wr), _ptr(alpha), _ptr(beta),
         _ptr(saved), _nbytes(saved), _ptr(dX), _ptr(dW), _ptr(dA), _ptr(dB), _ptr(dWr), _ptr(dalpha), _ptr(dbeta),
         _ptr(ws), _nbytes(ws), _stream(stream)))
+
+
+def _rows(fn, name, t, rows, width):
+    """Row stride in values of a 2-D (or packed, contiguous) bf16 tensor of `rows` rows of `width` values."""
+    if t.dtype != torch.bfloat16:
+        raise PqArgumentError(fn, f"{name} has to be bfloat16")
+    if t.dim() == 2 and t.shape[0] == rows and t.shape[1] == width and t.stride(1) == 1:
+        return t.stride(0) if rows > 1 else 0      # the stride of a single row means nothing
+    if t.is_contiguous() and t.numel() == rows * width:
+        return 0
+    raise PqArgumentError(fn, f"{name} has to hold {rows} rows of {width} values, each of them contiguous")
+
+
+def _need(fn, name, t, dtype, numel):
+    if t.dtype != dtype or t.numel() != numel or not t.is_contiguous():
+        raise PqArgumentError(fn, f"{name} has to be a contiguous tensor of {numel} {dtype} values")
+
+
+def _same_device(fn, *tensors):
+    """A kernel is launched on the current device: every tensor has to live there."""
+    dev = _device()
+    for t in tensors:
+        if t is not None and (t.device.type != "cuda" or t.device.index != dev):
+            raise PqArgumentError(fn, f"a tensor is on {t.device}, the current device is cuda:{dev}")
+
+
+def make_kv_cache(K, V, page_table, head_dim, k_gamma=None, v_gamma=None) -> pq_kv_cache:
+    """The cache whose pages are K, V [pages, heads, page_size, pitch] (bf16, or int8 with k_gamma, v_gamma [pages, heads,
+    page_size] fp32) and whose sequences' pages stand in page_table [sequences, entries] int32.  pitch = pq_kv_pitch(format, head_dim).
+    The struct only holds pointers: it keeps the tensors alive, and they must not be resized while it is in use."""
+    fn = "make_kv_cache"
+    int8 = K.dtype == torch.int8
+    if K.dim() != 4 or K.dtype not in (torch.bfloat16, torch.int8) or not K.is_contiguous():
+        raise PqArgumentError(fn, "K has to be a contiguous bfloat16 or int8 tensor [pages, heads, page_size, pitch]")
+    pages, heads, page_size, pitch = K.shape
+    if pitch != pq_kv_pitch(PQ_KV_INT8 if int8 else PQ_KV_BF16, head_dim):
+        raise PqArgumentError(fn, f"rows of {pitch} values do not fit heads of {head_dim}")
+    _need(fn, "V", V, K.dtype, K.numel())
+    if int8 != (k_gamma is not None) or int8 != (v_gamma is not None):
+        raise PqArgumentError(fn, "an int8 cache has k_gamma and v_gamma, a bfloat16 cache neither")
+    if int8:
+        _need(fn, "k_gamma", k_gamma, torch.float32, pages * heads * page_size)
+        _need(fn, "v_gamma", v_gamma, torch.float32, pages * heads * page_size)
+    if page_table.dim() != 2:
+        raise PqArgumentError(fn, "page_table has to be [sequences, entries]")
+    _need(fn, "page_table", page_table, torch.int32, page_table.numel())
+    if len({t.device for t in (K, V, page_table, k_gamma, v_gamma) if t is not None}) > 1:
+        raise PqArgumentError(fn, "the cache's tensors are on several devices")
+    c = pq_kv_cache(ctypes.sizeof(pq_kv_cache), 0, PQ_KV_INT8 if int8 else PQ_KV_BF16, heads, head_dim, page_size, pages, page_table.shape[0],
+                    page_table.shape[1], 0, K.data_ptr(), V.data_ptr(), k_gamma.data_ptr() if int8 else None, v_gamma.data_ptr() if int8 else None,
+                    page_table.data_ptr())
+    c.tensors = (K, V, page_table, k_gamma, v_gamma)
+    return c
+
+
+def pq_kv_pitch(format: int, head_dim: int) -> int:
+    return lib().pq_kv_pitch(format, head_dim)
+
+
+def pq_kv_append(cache, seq, pos, K, V, cos=None, sin=None, Q=None, Q_out=None, stream=None):
+    """Write tokens to the cache (rotated by cos, sin [rows, head_dim / 2] fp32 where given), and rotate their queries Q into Q_out.
+    K, V, Q: [tokens, heads * head_dim] bf16, rows of any stride; seq, pos: [tokens] int32."""
+    fn, n, width = "pq_kv_append", seq.numel(), cache.heads * cache.head_dim
+    _same_device(fn, cache.tensors[0], seq, pos, K, V, cos, sin, Q, Q_out)
+    _need(fn, "seq", seq, torch.int32, n)
+    _need(fn, "pos", pos, torch.int32, n)
+    rope_rows = q_heads = q_stride = 0
+    if cos is not None and sin is not None:
+        rope_rows = cos.numel() // (cache.head_dim // 2)
+        _need(fn, "cos", cos, torch.float32, rope_rows * (cache.head_dim // 2))
+        _need(fn, "sin", sin, torch.float32, cos.numel())
+    if Q is not None and Q_out is not None and n > 0:
+        q_heads = Q_out.numel() // (n * cache.head_dim)
+        _need(fn, "Q_out", Q_out, torch.bfloat16, n * q_heads * cache.head_dim)
+        q_stride = _rows(fn, "Q", Q, n, q_heads * cache.head_dim)
+    if n == 0:
+        return
+    _check(fn, lib().pq_kv_append(ctypes.byref(cache), n, _ptr(seq), _ptr(pos), _ptr(K), _rows(fn, "K", K, n, width), _ptr(V),
+                                  _rows(fn, "V", V, n, width), _ptr(cos), _ptr(sin), rope_rows, _ptr(Q), q_stride, q_heads, _ptr(Q_out),
+                                  _stream(stream)))
+
+
+def pq_kv_read(cache, seq, pos, K_out, V_out, stream=None):
+    """K_out, V_out [tokens, heads * head_dim] bf16: what the cache holds at (seq, pos)."""
+    fn, n = "pq_kv_read", seq.numel()
+    _same_device(fn, cache.tensors[0], seq, pos, K_out, V_out)
+    _need(fn, "seq", seq, torch.int32, n)
+    _need(fn, "pos", pos, torch.int32, n)
+    _need(fn, "K_out", K_out, torch.bfloat16, n * cache.heads * cache.head_dim)
+    _need(fn, "V_out", V_out, torch.bfloat16, n * cache.heads * cache.head_dim)
+    if n == 0:
+        return
+    _check(fn, lib().pq_kv_read(ctypes.byref(cache), n, _ptr(seq), _ptr(pos), _ptr(K_out), _ptr(V_out), _stream(stream)))
+
+
+def pq_attn_workspace_bytes(cache, q_heads: int) -> int:
+    return lib().pq_attn_workspace_bytes(ctypes.byref(cache), q_heads)
+
+
+def pq_attn_decode(cache, Q, lens, scale, O, lse, ws, stream=None):
+    """One token per sequence of the cache's page table: O [sequences, q_heads * head_dim] bf16 (and lse [sequences, q_heads] fp32, or None)
+    from Q of that shape (rows of any stride) over the first lens[s] positions."""
+    fn, n = "pq_attn_decode", cache.num_seqs
+    _same_device(fn, cache.tensors[0], Q, lens, O, lse, ws)
+    q_heads = O.numel() // (n * cache.head_dim)
+    _need(fn, "O", O, torch.bfloat16, n * q_heads * cache.head_dim)
+    _need(fn, "lens", lens, torch.int32, n)
+    if lse is not None:
+        _need(fn, "lse", lse, torch.float32, n * q_heads)
+    _check(fn, lib().pq_attn_decode(ctypes.byref(cache), q_heads, _ptr(Q), _rows(fn, "Q", Q, n, q_heads * cache.head_dim), _ptr(lens), scale, _ptr(O),
+                                    _ptr(lse), _ptr(ws), _nbytes(ws), _stream(stream)))
+
+
+def make_norm_desc(T, N, eps=1e-5, res_scale=1.0, gate_vector=False) -> pq_norm_desc:
+    return pq_norm_desc(ctypes.sizeof(pq_norm_desc), PQ_SCALE_VECTOR if gate_vector else 0, T, N, eps, res_scale)
+
+
+def _norm_arguments(fn, d, rows, weights, sums, gates):
+    _same_device(fn, *rows.values(), *weights.values(), *sums.values(), *gates.values())
+    for kind, dtype, numel in ((rows, torch.bfloat16, d.T * d.N), (weights, torch.bfloat16, d.N), (sums, torch.float32, d.N),
+                               (gates, torch.float32, d.N if d.flags & PQ_SCALE_VECTOR else 1)):
+        for name, t in kind.items():
+            if t is not None:
+                _need(fn, name, t, dtype, numel)
+
+
+def pq_block_norm_forward(d, x, y, post_weight, gate, pre_weight, x_out, h, stream=None):
+    """x_out = res_scale x + gate (rms(y) post_weight), h = rms(x_out) pre_weight; what is None is left out (see pquant.h)."""
+    _norm_arguments("pq_block_norm_forward", d, dict(x=x, y=y, x_out=x_out, h=h), dict(post_weight=post_weight, pre_weight=pre_weight), {}, dict(gate=gate))
+    _check("pq_block_norm_forward", lib().pq_block_norm_forward(ctypes.byref(d), _ptr(x), _ptr(y), _ptr(post_weight), _ptr(gate), _ptr(pre_weight),
+                                                                 _ptr(x_out), _ptr(h), _stream(stream)))
+
+
+def pq_block_norm_workspace_bytes(d: pq_norm_desc) -> int:
+    return lib().pq_block_norm_workspace_bytes(ctypes.byref(d))
+
+
+def pq_block_norm_backward(d, dx_out, dh, x_out, y, post_weight, gate, pre_weight, dx, dy, dpost, dgate, dpre, ws, stream=None):
+    """Gradients of pq_block_norm_forward; every one that is given is overwritten."""
+    _norm_arguments("pq_block_norm_backward", d, dict(dx_out=dx_out, dh=dh, x_out=x_out, y=y, dx=dx, dy=dy), dict(post_weight=post_weight, pre_weight=pre_weight),
+                    dict(dpost=dpost, dpre=dpre), dict(gate=gate, dgate=dgate))
+    _same_device("pq_block_norm_backward", ws)
+    _check("pq_block_norm_backward", lib().pq_block_norm_backward(
+        ctypes.byref(d), _ptr(dx_out), _ptr(dh), _ptr(x_out), _ptr(y), _ptr(post_weight), _ptr(gate), _ptr(pre_weight), _ptr(dx), _ptr(dy), _ptr(dpost),
+        _ptr(dgate), _ptr(dpre), _ptr(ws), _nbytes(ws), _stream(stream)))
 
 
 def pq_debug_gemm(mode, M, N, K, A, B, D, stream=None):

@@ -4,4 +4,7 @@
 #include "pq_gemm_kernels.cu"
 #include "pq_decode.cu"
 #include "pq_decode_stream.cu"
+#include "pq_kv.cu"
+#include "pq_attn.cu"
+#include "pq_norm.cu"
 #include "pq_api.cu"

@@ -224,6 +224,7 @@ const char* pq_status_string(int s) {
     case PQ_ERR_CUDA: return "a CUDA call failed";
     case PQ_ERR_TIMEOUT: return "a device-side bounded wait ran out";
     case PQ_ERR_TOO_LARGE: return "the problem needs more scratch than the library's fixed-size buffer holds";
+    case PQ_ERR_INDEX: return "an index in device memory is out of range";
     default: return "unknown status";
   }
 }
@@ -699,6 +700,125 @@ int pq_linear_backward(const pq_desc* d, const uint16_t* dY, const uint16_t* X, 
                              hp ? dalpha : nullptr, sc.blk_sums, sc.arrivals, st) != cudaSuccess)
     return PQ_ERR_CUDA;
   return PQ_OK;
+}
+
+// ---------------------------------------------------------------------------
+// Between the projections: key-value cache, attention over it, norms around a block
+// ---------------------------------------------------------------------------
+int pq_kv_pitch(int format, int head_dim) {
+  if ((format != PQ_KV_BF16 && format != PQ_KV_INT8) || head_dim < 8 || head_dim > 256 || head_dim % 4) return 0;
+  const int piece = format == PQ_KV_INT8 ? 16 : 8;
+  return (head_dim + piece - 1) / piece * piece;
+}
+
+// sizes alone: what a workspace query needs
+static int check_kv_sizes(const pq_kv_cache* c, KvCache* out) {
+  if (!c) return PQ_ERR_NULL;
+  if (c->size != sizeof(pq_kv_cache) || c->flags) return PQ_ERR_SHAPE;
+  const int pitch = pq_kv_pitch(c->format, c->head_dim);
+  if (!pitch || c->heads < 1 || c->page_size < 16 || c->page_size % 16 || c->num_pages < 1 || c->num_seqs < 1 || c->max_pages < 1) return PQ_ERR_SHAPE;
+  if ((int64_t)c->max_pages * c->page_size > INT32_MAX || (int64_t)c->num_seqs * c->heads > INT32_MAX / 256) return PQ_ERR_SHAPE;   // positions and items are ints
+  *out = KvCache{c->K, c->V, c->k_gamma, c->v_gamma, c->page_table, c->format, c->heads, c->head_dim, pitch, c->page_size, c->num_pages, c->num_seqs, c->max_pages};
+  return PQ_OK;
+}
+static int check_kv(const pq_kv_cache* c, KvCache* out) {
+  if (!c || !c->K || !c->V || !c->page_table) return PQ_ERR_NULL;
+  if (const int rc = check_kv_sizes(c, out)) return rc;
+  if (c->format == PQ_KV_INT8 && (!c->k_gamma || !c->v_gamma)) return PQ_ERR_NULL;
+  if (misaligned(c->K) || misaligned(c->V) || misaligned(c->k_gamma) || misaligned(c->v_gamma) || misaligned(c->page_table)) return PQ_ERR_ALIGN;
+  return PQ_OK;
+}
+// values from row to row; false where rows would overlap or their pieces lose their alignment
+static bool row_stride(int64_t given, int64_t dense, int64_t* out) {
+  *out = given ? given : dense;
+  return *out >= dense && *out % 4 == 0;
+}
+
+int pq_kv_append(const pq_kv_cache* c, int tokens, const int32_t* seq, const int32_t* pos, const uint16_t* K, int64_t k_stride,
+                 const uint16_t* V, int64_t v_stride, const float* cos, const float* sin, int rope_rows, const uint16_t* Q, int64_t q_stride,
+                 int q_heads, uint16_t* Q_out, void* stream) {
+  KvCache kv;
+  if (const int rc = check_kv(c, &kv)) return rc;
+  if (!seq || !pos || !K || !V || !cos != !sin || !Q != !Q_out) return PQ_ERR_NULL;
+  if (tokens < 0 || q_heads < 0 || (q_heads > 0) != (Q != nullptr) || q_heads > INT32_MAX / 512 || (cos && rope_rows < 1)) return PQ_ERR_SHAPE;
+  const int64_t dense = (int64_t)kv.heads * kv.dim, q_dense = (int64_t)q_heads * kv.dim;
+  if (!row_stride(k_stride, dense, &k_stride) || !row_stride(v_stride, dense, &v_stride) || (Q && !row_stride(q_stride, q_dense, &q_stride))) return PQ_ERR_SHAPE;
+  if (Q && Q_out == Q && q_stride != q_dense) return PQ_ERR_SHAPE;      // rows of the output would lie over other rows of the input
+  if (misaligned(seq) || misaligned(pos) || misaligned(K) || misaligned(V) || misaligned(cos) || misaligned(sin) || misaligned(Q) || misaligned(Q_out))
+    return PQ_ERR_ALIGN;
+  if (tokens == 0) return PQ_OK;
+  return launch_kv_append(kv, tokens, seq, pos, K, k_stride, V, v_stride, cos, sin, rope_rows, Q, q_stride, q_heads, Q_out,
+                          static_cast<cudaStream_t>(stream)) == cudaSuccess ? PQ_OK : PQ_ERR_CUDA;
+}
+
+int pq_kv_read(const pq_kv_cache* c, int tokens, const int32_t* seq, const int32_t* pos, uint16_t* K_out, uint16_t* V_out, void* stream) {
+  KvCache kv;
+  if (const int rc = check_kv(c, &kv)) return rc;
+  if (!seq || !pos || !K_out || !V_out) return PQ_ERR_NULL;
+  if (tokens < 0) return PQ_ERR_SHAPE;
+  if (misaligned(seq) || misaligned(pos) || misaligned(K_out) || misaligned(V_out)) return PQ_ERR_ALIGN;
+  if (tokens == 0) return PQ_OK;
+  return launch_kv_read(kv, tokens, seq, pos, K_out, V_out, static_cast<cudaStream_t>(stream)) == cudaSuccess ? PQ_OK : PQ_ERR_CUDA;
+}
+
+static bool q_heads_ok(const KvCache& kv, int q_heads) { return q_heads >= kv.heads && q_heads % kv.heads == 0 && q_heads <= INT32_MAX / 512; }
+
+size_t pq_attn_workspace_bytes(const pq_kv_cache* c, int q_heads) {
+  KvCache kv;
+  if (check_kv_sizes(c, &kv) != PQ_OK || !q_heads_ok(kv, q_heads)) return 0;
+  return attn_workspace_bytes(kv, q_heads);
+}
+
+int pq_attn_decode(const pq_kv_cache* c, int q_heads, const uint16_t* Q, int64_t q_stride, const int32_t* lens, float scale, uint16_t* O,
+                   float* lse, void* ws, size_t ws_bytes, void* stream) {
+  KvCache kv;
+  if (const int rc = check_kv(c, &kv)) return rc;
+  if (!Q || !lens || !O || !ws) return PQ_ERR_NULL;
+  if (!q_heads_ok(kv, q_heads) || !row_stride(q_stride, (int64_t)q_heads * kv.dim, &q_stride)) return PQ_ERR_SHAPE;
+  if (!(scale - scale == 0.f)) return PQ_ERR_SHAPE;      // infinite or not a number
+  if (misaligned(Q) || misaligned(lens) || misaligned(O) || misaligned(lse) || misaligned(ws)) return PQ_ERR_ALIGN;
+  if (ws_bytes < attn_workspace_bytes(kv, q_heads)) return PQ_ERR_WORKSPACE;
+  return launch_attn_decode(kv, q_heads, Q, q_stride, lens, scale, O, lse, ws, static_cast<cudaStream_t>(stream)) == cudaSuccess ? PQ_OK : PQ_ERR_CUDA;
+}
+
+static int check_norm_desc(const pq_norm_desc* d) {
+  if (!d) return PQ_ERR_NULL;
+  if (d->size != sizeof(pq_norm_desc) || (d->flags & ~(uint32_t)PQ_SCALE_VECTOR)) return PQ_ERR_SHAPE;
+  if (d->T < 1 || d->N < 8 || d->N % 8 || d->N > 16384) return PQ_ERR_SHAPE;
+  if (!(d->eps > 0.f) || !(d->eps - d->eps == 0.f) || !(d->res_scale - d->res_scale == 0.f)) return PQ_ERR_SHAPE;
+  return PQ_OK;
+}
+
+int pq_block_norm_forward(const pq_norm_desc* d, const uint16_t* x, const uint16_t* y, const uint16_t* post_weight, const float* gate,
+                          const uint16_t* pre_weight, uint16_t* x_out, uint16_t* h, void* stream) {
+  if (const int rc = check_norm_desc(d)) return rc;
+  if (!x || (!x_out && !h) || !pre_weight != !h || (!y && (post_weight || gate))) return PQ_ERR_NULL;
+  if (misaligned(x) || misaligned(y) || misaligned(post_weight) || misaligned(gate) || misaligned(pre_weight) || misaligned(x_out) || misaligned(h))
+    return PQ_ERR_ALIGN;
+  BlockNormArgs a{};
+  a.T = d->T; a.N = d->N; a.eps = d->eps; a.res_scale = d->res_scale; a.gate_vector = gate && (d->flags & PQ_SCALE_VECTOR);
+  a.x = x; a.y = y; a.post = post_weight; a.pre = pre_weight; a.gate = gate; a.x_out = x_out; a.h = h;
+  return launch_block_norm_forward(a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? PQ_OK : PQ_ERR_CUDA;
+}
+
+size_t pq_block_norm_workspace_bytes(const pq_norm_desc* d) { return check_norm_desc(d) == PQ_OK ? block_norm_workspace_bytes(d->T, d->N) : 0; }
+
+int pq_block_norm_backward(const pq_norm_desc* d, const uint16_t* dx_out, const uint16_t* dh, const uint16_t* x_out, const uint16_t* y,
+                           const uint16_t* post_weight, const float* gate, const uint16_t* pre_weight, uint16_t* dx, uint16_t* dy, float* dpost,
+                           float* dgate, float* dpre, void* ws, size_t ws_bytes, void* stream) {
+  if (const int rc = check_norm_desc(d)) return rc;
+  if ((!dx_out && !dh) || !dx || !ws || !dh != !pre_weight || (dh && (!x_out || !dpre))) return PQ_ERR_NULL;
+  if ((post_weight || gate) && (!y || !dy)) return PQ_ERR_NULL;
+  if ((post_weight && !dpost) || (gate && !dgate)) return PQ_ERR_NULL;
+  if (misaligned(dx_out) || misaligned(dh) || misaligned(x_out) || misaligned(y) || misaligned(post_weight) || misaligned(gate) || misaligned(pre_weight) ||
+      misaligned(dx) || misaligned(dy) || misaligned(dpost) || misaligned(dgate) || misaligned(dpre) || misaligned(ws))
+    return PQ_ERR_ALIGN;
+  if (ws_bytes < block_norm_workspace_bytes(d->T, d->N)) return PQ_ERR_WORKSPACE;
+  BlockNormArgs a{};
+  a.T = d->T; a.N = d->N; a.eps = d->eps; a.res_scale = d->res_scale; a.gate_vector = gate && (d->flags & PQ_SCALE_VECTOR);
+  a.x = x_out; a.y = y; a.post = post_weight; a.pre = pre_weight; a.gate = gate;
+  a.dx_out = dx_out; a.dh = dh; a.dx = dx; a.dy = dy; a.dpost = dpost; a.dgate = dgate; a.dpre = dpre;
+  return launch_block_norm_backward(a, ws, static_cast<cudaStream_t>(stream)) == cudaSuccess ? PQ_OK : PQ_ERR_CUDA;
 }
 
 int pq_debug_gemm(int mode, int M, int N, int K, const void* A, const void* B, void* D, void* stream) {

@@ -17,7 +17,8 @@ constexpr float kActAmaxFloor = 1e-5f;     // all-zero row guard
 enum KernelId : int {
   KID_PACK_SUMS = 0, KID_BINARIZE_PACK, KID_ROUTER, KID_ROUTE_SCAN, KID_ACT_QUANT, KID_HP_UP, KID_FWD, KID_SCATTER_ROWS,
   KID_SCALED_SIGN, KID_BWD_DW = 12, KID_SUM_PARTIALS = 16, KID_SUM_SCALAR, KID_DEBUG, KID_DECODE_PREP, KID_DECODE_MAIN,
-  KID_DECODE_PACK = 23, KID_DECODE_STREAM, KID_COUNT
+  KID_DECODE_PACK = 23, KID_DECODE_STREAM, KID_KV_APPEND, KID_KV_READ, KID_ATTN_DECODE, KID_ATTN_JOIN, KID_NORM_FWD, KID_NORM_BWD, KID_NORM_SUMS,
+  KID_COUNT
 };
 struct ProfileSlot { cudaEvent_t start, stop; };
 extern ProfileSlot g_profile[KID_COUNT];
@@ -83,12 +84,12 @@ inline int sm_count() {
 // griddepcontrol.launch_dependents and griddepcontrol.wait, i.e. touches no global memory before the predecessor
 // has completed; the result is the launch's, and is also left for the caller's cudaGetLastError().
 template <class... KArgs, class... Args>
-inline cudaError_t launch_pdl(void (*kernel)(KArgs...), int grid, int block, size_t smem, cudaStream_t st, Args&&... args) {
+inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, cudaStream_t st, Args&&... args) {
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)grid, 1, 1); cfg.blockDim = dim3((unsigned)block, 1, 1); cfg.dynamicSmemBytes = smem;
+  cfg.gridDim = grid; cfg.blockDim = dim3((unsigned)block, 1, 1); cfg.dynamicSmemBytes = smem;
   cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
@@ -164,6 +165,39 @@ int decode_batch(const DecodeItemArgs* items, int n, cudaStream_t st);   // inde
 void decode_set_pdl(int on);
 void decode_set_poll(int on);           // waits without suspension (a spin limit of a few cycles)
 DecodeViewPtrs decode_view(int M, int K, int N, int r, void* ws, bool dump);
+
+// paged key-value cache (pq_kv.cu): pages of [head][position][pitch] for keys and for values
+struct KvCache {
+  void* K; void* V;               // bf16 or int8 (format)
+  float* k_gamma; float* v_gamma; // int8: [page][head][position]
+  const int* page_table;          // [num_seqs][max_pages]
+  int format, heads, dim, pitch, page_size, num_pages, num_seqs, max_pages;
+};
+cudaError_t launch_kv_append(const KvCache& c, int tokens, const int* seq, const int* pos, const uint16_t* K, long long k_stride,
+                             const uint16_t* V, long long v_stride, const float* cos_t, const float* sin_t, int rope_rows, const uint16_t* Q,
+                             long long q_stride, int q_heads, uint16_t* Q_out, cudaStream_t st);
+cudaError_t launch_kv_read(const KvCache& c, int tokens, const int* seq, const int* pos, uint16_t* K_out, uint16_t* V_out, cudaStream_t st);
+// attention of one token per sequence over it (pq_attn.cu)
+size_t attn_workspace_bytes(const KvCache& c, int q_heads);
+cudaError_t launch_attn_decode(const KvCache& c, int q_heads, const uint16_t* Q, long long q_stride, const int* lens, float scale, uint16_t* O, float* lse,
+                               void* ws, cudaStream_t st);
+// norms around a block (pq_norm.cu)
+struct BlockNormArgs {
+  int T, N;
+  float eps, res_scale;
+  int gate_vector;
+  const uint16_t *x, *y, *post, *pre;   // x: the stream in front of the block (forward), behind it (backward)
+  const float* gate;
+  // forward
+  uint16_t *x_out, *h;
+  // backward
+  const uint16_t *dx_out, *dh;
+  uint16_t *dx, *dy;
+  float *dpost, *dgate, *dpre;
+};
+cudaError_t launch_block_norm_forward(const BlockNormArgs& a, cudaStream_t st);
+size_t block_norm_workspace_bytes(int T, int N);
+cudaError_t launch_block_norm_backward(const BlockNormArgs& a, void* ws, cudaStream_t st);
 
 struct BwdBuffers {
   const uint16_t* dys;   // [T,N] bf16 upstream gradient in sorted order
