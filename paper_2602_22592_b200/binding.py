@@ -32,8 +32,8 @@ EXPORTS = ("pq_status_string", "pq_workspace_bytes", "pq_saved_bytes", "pq_saved
 
 KERNEL_IDS = dict(pack_sums=0, binarize_pack=1, router=2, route_scan=3, act_quant=4, hp_up=5, fwd=6, scatter_rows=7,
                   scaled_sign=8, bwd_dw=12, sum_partials=16, sum_scalar=17, debug=18, decode_prep=19, decode_main=20,
-                  decode_pack=23, decode_stream=24, kv_append=25, kv_read=26, attn_decode=27, attn_join=28, norm_fwd=29,
-                  norm_bwd=30, norm_sums=31)
+                  decode_pack=23, decode_stream=24, kv_append=25, kv_read=26, attn_decode=27, norm_fwd=28,
+                  norm_bwd=29, norm_sums=30)
 
 
 class PqError(RuntimeError):

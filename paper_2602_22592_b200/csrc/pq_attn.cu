@@ -4,21 +4,28 @@
 // A pass reads every cached row once and multiplies it with the group x head_dim query values that share its head: one to
 // sixteen multiplications per byte, far below what the tensor cores need to be the limit, so that the memory is.  What
 // follows from that:
-//   * A warp works alone.  It walks tiles of sixteen positions; all loads of a tile are 16-byte asynchronous copies into a ring
-//     that is private to each LANE (a lane copies exactly the pieces that it will multiply), so that nothing is shared, no barrier
-//     is met and no bank conflicts: the ring (about 200 KB per SM) is the latency cover.
-//   * The work is cut into equal shares of tiles per warp over ALL sequences and heads (lengths live on the device: every CTA
-//     sums them itself), so that ragged batches, one long sequence and many short ones all keep every SM reading until the
-//     end.  A (sequence, head) cut between warps leaves partial sums, which k_attn_join adds.
+//   * A warp works alone while it reads: it walks tiles of sixteen positions, copies them asynchronously in whole lines (a copy of a
+//     warp is 512 neighbouring bytes; 16 bytes here and there in eight rows at once reached 4.5 TB/s, lines reach 5.9) into a ring
+//     of its own, and meets no barrier.  The ring, 200 KB per SM, covers the latency.  Its 16-byte pieces are swizzled, so that
+//     ldmatrix reads them without bank conflicts.
+//   * The work is cut into equal shares of tiles per CTA, and within it per warp, over ALL sequences and heads (lengths live on the
+//     device: every CTA adds them up itself), so that ragged batches, one long sequence and many short ones all keep every SM
+//     reading until the end.  What a (sequence, head) cut between warps leaves is joined in the CTA, what one cut between CTAs
+//     leaves by the CTA that arrives last, in the order of the positions: one launch, and the same bits whoever is last.
 //   * S^T = K q^T on mma.sync.m16n8k16: positions are the sixteen rows, query heads the eight columns (two column blocks for
-//     nine to sixteen).  tcgen05 has no shape for eight columns by sixteen rows that would not idle.  The contraction index may
-//     be permuted at will as long as both operands agree: a lane's 16 bytes of a key row are eight neighbouring values, so that
-//     cache rows stay in their natural order.  O^T = V^T P^T the same way: a lane holds four positions of the same dims, byte
-//     permutes pair neighbouring positions.
-//   * P enters the second product as the sum of two bf16 numbers (2^-17 relative): the tensor cores have room, and a single
-//     rounding of P would be as large as the output's own.  int8 codes are exact in bf16; gamma_k scales the scores and
-//     1 / gamma_v the weights, in fp32.
-#include <algorithm>
+//     nine to sixteen).  tcgen05 has no shape for eight columns by sixteen rows that would not idle.  O^T = V^T P^T with V^T by
+//     transposed ldmatrix.  Of int8 rows a 16-bit element is two codes, neighbours in a row: the contraction index of K and the
+//     rows of V^T are permuted accordingly, queries and outputs with them.
+//   * Types of the products.  A bf16 cache multiplies in bf16, and the weights enter the second product as the sum of two bf16
+//     numbers (2^-17 relative): a single rounding of them would be as large as the output's own.  An int8 cache multiplies in
+//     fp16, where codes are exact and cost least to make: queries are scaled by a power of two per row (exact: bf16 has
+//     fewer bits), and the weights, 2^14 at most, are rounded once to eleven bits, an eighth of the output's rounding.  gamma_k
+//     scales the scores; the weights are taken with their 1 / gamma_v inside the exponent, exp2(s - log2 gamma_v - m), m the
+//     maximum of that, so that they stay in range, and the sum of weights puts gamma_v back.
+#include <cuda_fp16.h>
+
+#include <atomic>
+#include <chrono>
 #include <mutex>
 
 #include "pq_kernels.cuh"
@@ -26,51 +33,70 @@
 namespace pq {
 
 constexpr int kAttnTile = 16;                 // positions of a tile; pages are multiples of it
-constexpr int kAttnRingBytes = 200 * 1024;
+constexpr int kAttnRingBytes = 208 * 1024;
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
 template <int DP, int NT, bool I8>
 struct AttnForm {
-  static constexpr int kWarps = DP == 256 ? 4 : 8;
-  static constexpr int kK = I8 ? DP / 64 : DP / 32;                    // 16-byte pieces of a key row per lane (four lanes a row)
-  static constexpr int kV = I8 ? (DP + 127) / 128 : DP / 64;           // pieces of a value row per lane (eight lanes a row)
-  static constexpr int kVBytes = I8 && DP == 64 ? 8 : 16;              // ... and their size
-  static constexpr int kSlots = 2 * kK + 4 * kV + (I8 ? 1 : 0);        // ring places of 16 bytes x 32 lanes of a stage
-  static constexpr int kStageBytes = kSlots * 512;
-  static constexpr int kFit = kAttnRingBytes / (kStageBytes * kWarps);
+  static constexpr int kRow = DP * (I8 ? 1 : 2);                       // bytes of a row in the ring
+  static constexpr int kChunks = kRow / 16;                            // ... and its 16-byte pieces
+  static constexpr int kTileBytes = kAttnTile * kRow;                  // keys of a tile; values behind them
+  static constexpr int kCopies = kTileBytes / 512;                     // copies of a warp for a tile's keys
+  static constexpr int kStageBytes = 2 * kTileBytes;
+  static constexpr int kGammaBytes = I8 ? 128 : 0;                     // 16 of the keys, 16 of the values
+  // As many warps as registers allow: sixteen where accumulators and queries fit in 128
+  static constexpr int kWarps = DP * NT <= 128 && kStageBytes <= 4096 ? 16 : kStageBytes <= 8192 ? 8 : 4;
+  static constexpr int kFit = kAttnRingBytes / ((kStageBytes + kGammaBytes) * kWarps);
   static constexpr int kStages = kFit > 6 ? 6 : kFit;
-  static constexpr int kSmem = kStages * kStageBytes * kWarps;
+  static constexpr int kGammaAt = kStages * kStageBytes * kWarps;      // the gammas behind all rings
+  static constexpr int kSmem = kGammaAt + kStages * kGammaBytes * kWarps;
   static_assert(kStages >= 3, "two stages in flight and one in use");
+  static_assert(8 * NT * DP * 4 <= kStages * kStageBytes, "a warp's last partial sums fit in its ring");
 };
-
-__device__ __forceinline__ void attn_copy8(uint32_t dst, const void* src, bool valid) {      // zeros where not valid: nothing is read
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(valid ? 8 : 0) : "memory");
+// Where piece c of row r lies in a tile: the eight rows that ldmatrix reads at once fall into eight different bank groups
+template <int ROW>
+__device__ __forceinline__ uint32_t attn_place(int r, int c) {
+  return r * ROW + ((c ^ (ROW >= 128 ? r & 7 : r >> 1 & 3)) << 4);
 }
+
 __device__ __forceinline__ void attn_copy4(uint32_t dst, const void* src, bool valid) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(valid ? 4 : 0) : "memory");
 }
 __device__ __forceinline__ void attn_copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void attn_copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ uint4 attn_lds128(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
-  return v;
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float attn_exp2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float attn_log2(float x) { float y; asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float attn_rcp(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ void ldmatrix4(uint32_t at, uint32_t (&v)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t at, uint32_t (&v)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(at) : "memory");
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   uint32_t r;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
-// Four int8 codes -> two pairs of bf16, exactly: behind an exponent byte 0x43 the low seven bits read 128 + low, the sign bit
-// alone 128 or 256, and the difference is the code.
-__device__ __forceinline__ uint32_t codes_to_bf16(uint32_t halves) {
-  const uint32_t a = halves & 0xFF7FFF7Fu, b = halves & 0xFF80FF80u;
-  const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+// Four int8 codes with their sign bits flipped (0 to 255) -> two pairs of fp16: behind an exponent byte 0x64 they read 1024 + u,
+// and 1152 less is the code
+__device__ __forceinline__ uint32_t codes_to_f16(uint32_t halves) {
+  const uint32_t bias = 0xE480E480u;      // -1152, twice
+  const __half2 r = __hadd2(*reinterpret_cast<const __half2*>(&halves), *reinterpret_cast<const __half2*>(&bias));
   return *reinterpret_cast<const uint32_t*>(&r);
 }
-__device__ __forceinline__ uint32_t codes_lo(uint32_t w) { return codes_to_bf16(__byte_perm(w, 0x43434343u, 0x4140)); }
-__device__ __forceinline__ uint32_t codes_hi(uint32_t w) { return codes_to_bf16(__byte_perm(w, 0x43434343u, 0x4342)); }
+template <int SEL>      // which two bytes
+__device__ __forceinline__ uint32_t codes_pair(uint32_t flipped) { return codes_to_f16(__byte_perm(flipped, 0x64646464u, SEL)); }
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+constexpr float kWeightTop = 14.f;        // int8 caches: the largest weight is 2^14, so that small ones keep their bits in fp16
 
 struct AttnArgs {
   KvCache c;
@@ -83,26 +109,29 @@ struct AttnArgs {
   int q_heads, group;        // query heads, and of them per cache head
   int blocks;                // column blocks of 8 NT query heads per cache head
   // workspace
-  float* part;               // [2 teams][8 NT][DP] unnormalised sums, ...
-  float2* part_ml;           // [2 teams][8 NT] ... their maximum (in powers of two) and sum of weights
-  int4* head;                // [min(teams, items)] what k_attn_join has to add: {first slot, pieces, item, -} or pieces = 0
-  int teams;                 // warps of the launch
-  int head_by_item;          // head's index is the item (else the team that holds its beginning)
+  float* warp_part;          // [CTAs x warps][8 NT][DP] unnormalised sums of a warp's first piece, if that is not its last
+  float* cta_part;           // [2 CTAs][8 NT][DP] the same of a CTA: 2 c + 1 where its piece is the item's beginning, 2 c elsewhere
+  float2* cta_ml;            // [2 CTAs][8 NT] what was taken off the scores, and the sum of weights
+  unsigned long long* arrived;   // [CTAs] of the item that begins in the CTA: how many of its pieces are there, marked with `call`
+  unsigned long long call;   // a number of this launch, above 16 bits: what the workspace held before is recognised by its absence
 };
 
-__device__ __forceinline__ int attn_len(const AttnArgs& a, int seq) {
-  return min(__ldcg(a.lens + seq), a.c.max_pages * a.c.page_size);       // longer: reported where the lengths are added up
+constexpr int kAttnLens = 1024;      // lengths kept in shared memory
+
+__device__ __forceinline__ int attn_len(const AttnArgs& a, const int* lens, int seq) {
+  const int len = a.c.num_seqs <= kAttnLens ? lens[seq] : __ldcg(a.lens + seq);
+  return min(len, a.c.max_pages * a.c.page_size);       // longer: reported where the lengths are added up
 }
 
-// A walk over a team's share: its segments are stretches of tiles of one item = (sequence, cache head, column block).
+// A walk over a warp's share: its segments are stretches of tiles of one item = (sequence, cache head, column block).
 struct AttnWalk {
   long long left;            // tiles of the share behind the current segment
   int seq, hb, t0, t1, len, tiles;
-  __device__ bool next(const AttnArgs& a, int per_seq) {
+  __device__ bool next(const AttnArgs& a, const int* lens, int per_seq) {
     if (left <= 0) return false;
     if (++hb == per_seq) {
       hb = 0;
-      do { len = attn_len(a, ++seq); } while (len <= 0);
+      do { len = attn_len(a, lens, ++seq); } while (len <= 0);
       tiles = (len + kAttnTile - 1) / kAttnTile;
     }
     t0 = 0;
@@ -112,51 +141,77 @@ struct AttnWalk {
   }
 };
 
+// One piece of a cut item: what a warp leaves for the CTA's join
+struct AttnPiece {
+  int item;                  // -1: none
+  int seq, hb, whole_from, whole_to;   // whether the item begins, ends here
+};
+
+__device__ __forceinline__ void attn_store(const AttnArgs& a, long long qrow, int dim, float v0, float v1, float v2, float v3, float inv) {
+  *reinterpret_cast<uint2*>(a.O + qrow * a.c.dim + dim) = make_uint2(pack_bf16x2(v0 * inv, v1 * inv), pack_bf16x2(v2 * inv, v3 * inv));
+}
+__device__ __forceinline__ float attn_inv(float l) { return l == 0.f ? 0.f : 1.f / l; }      // no weight: zeros
+__device__ __forceinline__ float attn_lse(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2; }
+
 template <int DP, int NT, bool I8>
 __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_decode(const __grid_constant__ AttnArgs a) {
   using F = AttnForm<DP, NT, I8>;
-  constexpr int kThreads = F::kWarps * 32, kQ = 8 * NT;
-  extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ long long sums[kThreads + 1];      // tiles of the sequences before a thread's own
-  __shared__ long long warp_sums[F::kWarps];
+  constexpr int kWarps = F::kWarps, kThreads = kWarps * 32, kQ = 8 * NT;
+  extern __shared__ __align__(1024) uint8_t attn_smem[];      // a name of its own: the swizzle needs this alignment, a shared name takes the first one seen
+  uint8_t* const smem = attn_smem;
+  __shared__ long long sums[kThreads];          // tiles of the sequences before a thread's own
+  __shared__ long long warp_sums[kWarps];
+  __shared__ int lens[kAttnLens];
+  __shared__ AttnPiece pieces[2 * kWarps];
+  __shared__ float2 piece_ml[2 * kWarps][kQ];   // {taken off the scores, -infinity without weight; sum of weights}
+  __shared__ int arrived_last;
   pdl_launch_dependents();
   pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const int per_seq = a.c.heads * a.blocks, n = a.c.num_seqs;
-  // ---- shares: every CTA adds up the lengths
+  // ---- shares: every CTA adds up the lengths.  chunks: what the items would be in pieces of one tile per warp, the least that a CTA
+  // is worth waking for
   const int per = (n + kThreads - 1) / kThreads;
-  long long mine = 0;
+  long long mine = 0, mine_chunks = 0;
   for (int i = 0; i < per; ++i) {
     const int s = tid * per + i;
     if (s >= n) break;
     const int raw = __ldcg(a.lens + s);
+    if (n <= kAttnLens) lens[s] = raw;
     if (raw > a.c.max_pages * a.c.page_size && blockIdx.x == 0) report_index();
-    mine += (max(0, attn_len(a, s)) + kAttnTile - 1) / kAttnTile;
+    const int tiles = (max(0, min(raw, a.c.max_pages * a.c.page_size)) + kAttnTile - 1) / kAttnTile;
+    mine += tiles;
+    mine_chunks += (tiles + kWarps - 1) / kWarps;
   }
   long long upto = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
     const long long v = __shfl_up_sync(0xffffffffu, upto, d);
     if (lane >= d) upto += v;
+    mine_chunks += __shfl_xor_sync(0xffffffffu, mine_chunks, d);
   }
-  if (lane == 31) warp_sums[warp] = upto;
+  __shared__ long long warp_chunks[kWarps];
+  if (lane == 31) { warp_sums[warp] = upto; warp_chunks[warp] = mine_chunks; }
+  if (tid < 2 * kWarps) pieces[tid].item = -1;
   __syncthreads();
-  long long before = 0, total = 0;
+  long long before = 0, total = 0, chunks_all = 0;
 #pragma unroll
-  for (int w = 0; w < F::kWarps; ++w) {
+  for (int w = 0; w < kWarps; ++w) {
     if (w < warp) before += warp_sums[w];
     total += warp_sums[w];
+    chunks_all += warp_chunks[w];
   }
   sums[tid] = before + upto - mine;
   __syncthreads();
   const long long tiles_all = total * per_seq;
-  const int team = warp * gridDim.x + blockIdx.x;            // few teams with work: one per SM
-  const long long used = tiles_all < a.teams ? tiles_all : a.teams;
-  const long long r0 = team < used ? team * tiles_all / used : 0, r1 = team < used ? (team + 1) * tiles_all / used : 0;
-  bool headed = false;                                        // head[team] written
+  chunks_all *= per_seq;
+  const int cta = blockIdx.x, used = (int)(chunks_all < gridDim.x ? chunks_all : gridDim.x);
+  const long long c0 = cta < used ? cta * tiles_all / used : 0, c1 = cta < used ? (cta + 1) * tiles_all / used : 0;
+  const long long r0 = c0 + (c1 - c0) * warp / kWarps, r1 = c0 + (c1 - c0) * (warp + 1) / kWarps;
+  uint8_t* const ring = smem + warp * (F::kStages * F::kStageBytes);
   if (r0 < r1) {
     // ---- first segment: the sequence whose tiles hold r0
-    const long long x = r0 / per_seq;                         // sums[.] <= x: compared per sequence, not per head
+    const long long x = r0 / per_seq;                         // compared per sequence, not per head
     int lo = 0, hi = kThreads;                                // last thread whose sequences begin at or before it
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
@@ -166,7 +221,7 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
     long long base = sums[lo];
     cw.seq = lo * per;
     for (;; ++cw.seq) {
-      cw.len = attn_len(a, cw.seq);
+      cw.len = attn_len(a, lens, cw.seq);
       cw.tiles = (max(0, cw.len) + kAttnTile - 1) / kAttnTile;
       if (x < base + cw.tiles) break;
       base += cw.tiles;
@@ -177,141 +232,209 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
     cw.t1 = (int)(cw.tiles - cw.t0 < r1 - r0 ? cw.tiles : cw.t0 + (r1 - r0));
     cw.left = r1 - r0 - (cw.t1 - cw.t0);
     AttnWalk pw = cw;                                         // the loads run ahead of the products, across segments
-    int pt = cw.t0;
+    int pt = cw.t0, run = 0;                                  // next tile to load, and how many more of its page
     bool more = true;
-    const int tiles_per_page = a.c.page_size / kAttnTile;
-    const uint32_t ring = smem_u32(smem) + warp * (F::kStages * F::kStageBytes) + lane * 16;
-    const int row_bytes = a.c.pitch * (I8 ? 1 : 2);
+    long long row0 = 0;                                       // its first row
+    const int tiles_per_page = a.c.page_size / kAttnTile, row_bytes = a.c.pitch * (I8 ? 1 : 2), chunks = row_bytes / 16;
+    const uint32_t ring_at = smem_u32(ring), gamma_at = smem_u32(smem) + F::kGammaAt + warp * (F::kStages * F::kGammaBytes);
+    // copy i takes this lane's piece 32 i + lane of the tile, whose rows are neighbours in the page
+    uint32_t place[F::kCopies];
+#pragma unroll
+    for (int i = 0; i < F::kCopies; ++i) {
+      const int at = 32 * i + lane, r = at / chunks;
+      place[i] = attn_place<F::kRow>(r, at - r * chunks);
+    }
+    if (chunks < F::kChunks) {                                // pieces behind the rows' end are never copied: zeros once and for all
+      for (int s = 0; s < F::kStages; ++s)
+        for (int i = lane; i < kAttnTile * F::kChunks; i += 32)
+          if (i % F::kChunks >= chunks)
+            *reinterpret_cast<uint4*>(ring + s * F::kStageBytes + attn_place<F::kRow>(i / F::kChunks, i % F::kChunks)) = make_uint4(0, 0, 0, 0);
+    }
     auto page_of = [&]() { return __ldcg(a.c.page_table + (long long)pw.seq * a.c.max_pages + pt / tiles_per_page); };
     int page = page_of();                                     // of tile pt, asked for a tile ahead
     auto issue = [&](int stage) {
       if (more) {
-        const bool known = (unsigned)page < (unsigned)a.c.num_pages;
-        if (!known && lane == 0) report_index();
-        const int rows = known ? min(kAttnTile, pw.len - pt * kAttnTile) : 0;
-        const int head = pw.hb / a.blocks;
-        const long long row0 = known ? ((long long)page * a.c.heads + head) * a.c.page_size + (pt % tiles_per_page) * kAttnTile : 0;
-        const uint8_t* kp = static_cast<const uint8_t*>(a.c.K) + row0 * row_bytes;
-        const uint8_t* vp = static_cast<const uint8_t*>(a.c.V) + row0 * row_bytes;
-        uint32_t dst = ring + stage * F::kStageBytes;
+        bool known = true;
+        if (run == 0) {                                       // another page
+          known = (unsigned)page < (unsigned)a.c.num_pages;
+          if (!known && lane == 0) report_index();
+          const int in_page = pt % tiles_per_page;
+          run = known ? min(tiles_per_page - in_page, pw.t1 - pt) : 1;
+          row0 = known ? ((long long)page * a.c.heads + pw.hb / a.blocks) * a.c.page_size + in_page * kAttnTile : 0;
+        }
+        const int rows = known ? pw.len - pt * kAttnTile : 0;
+        const uint8_t* const kp = static_cast<const uint8_t*>(a.c.K) + row0 * row_bytes + lane * 16;
+        const uint8_t* const vp = static_cast<const uint8_t*>(a.c.V) + row0 * row_bytes + lane * 16;
+        const uint32_t dst = ring_at + stage * F::kStageBytes;
+        const int have = min(rows, kAttnTile) * chunks - lane;            // this lane's pieces: 32 i < have
+        if (rows >= kAttnTile) {
 #pragma unroll
-        for (int j = 0; j < F::kK; ++j)
+          for (int i = 0; i < F::kCopies; ++i)
+            if (32 * i < have) cp_async16(dst + place[i], kp + 512 * i, true);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int row = g + 8 * h, at = j * 64 + t * 16;
-            const bool ok = row < rows && at < row_bytes;
-            cp_async16(dst, kp + (ok ? row * row_bytes + at : 0), ok);
-            dst += 512;
-          }
+          for (int i = 0; i < F::kCopies; ++i)
+            if (32 * i < have) cp_async16(dst + F::kTileBytes + place[i], vp + 512 * i, true);
+        } else {                                              // the sequence ends inside: rows behind its end are zero, and not read
 #pragma unroll
-        for (int j = 0; j < F::kV; ++j)
-#pragma unroll
-          for (int h = 0; h < 4; ++h) {
-            const int row = 2 * t + (h & 1) + (h >> 1) * 8, at = j * 8 * F::kVBytes + g * F::kVBytes;
-            const bool ok = row < rows && at < row_bytes;
-            if constexpr (F::kVBytes == 16) cp_async16(dst, vp + (ok ? row * row_bytes + at : 0), ok);
-            else attn_copy8(dst, vp + (ok ? row * row_bytes + at : 0), ok);
-            dst += 512;
-          }
+          for (int i = 0; i < F::kCopies; ++i)
+            if (32 * i + lane < kAttnTile * chunks) {
+              const bool ok = 32 * i < have;
+              cp_async16(dst + place[i], ok ? kp + 512 * i : static_cast<const uint8_t*>(a.c.K), ok);
+              cp_async16(dst + F::kTileBytes + place[i], ok ? vp + 512 * i : static_cast<const uint8_t*>(a.c.V), ok);
+            }
+        }
         if constexpr (I8) {
-#pragma unroll
-          for (int h = 0; h < 4; ++h) {
-            const int row = g + 8 * (h & 1);
-            const bool ok = row < rows;
-            attn_copy4(dst + 4 * h, (h < 2 ? a.c.k_gamma : a.c.v_gamma) + (ok ? row0 + row : 0), ok);
+          const int r = lane & 15;
+          attn_copy4(gamma_at + stage * F::kGammaBytes + lane * 4, (lane < 16 ? a.c.k_gamma : a.c.v_gamma) + (r < rows ? row0 + r : 0), r < rows);
+        }
+        row0 += kAttnTile;
+        ++pt;
+        if (--run == 0) {
+          if (pt == pw.t1) {
+            more = pw.next(a, lens, per_seq);
+            pt = pw.t0;
           }
+          if (more) page = page_of();
         }
-        if (++pt == pw.t1) {
-          more = pw.next(a, per_seq);
-          pt = pw.t0;
-        }
-        if (more) page = page_of();
       }
       attn_copy_commit();
     };
 #pragma unroll
     for (int s = 0; s < F::kStages - 1; ++s) issue(s);
     int stage = 0, ahead = F::kStages - 1;
+    // ldmatrix addresses: of the keys the matrices (rows 0-7, 8-15) of a piece, then of the next one; of the values (transposed) the same
+    // by pieces first for bf16, whose m-tiles are two pieces, by rows first for int8, whose m-tile is one
+    const int mr = lane & 7, m1 = lane >> 3 & 1, m2 = lane >> 4;
+    const uint32_t k_mat = attn_place<F::kRow>(mr + 8 * m1, m2);
+    const uint32_t v_mat = F::kTileBytes + (I8 ? attn_place<F::kRow>(mr + 8 * m1, m2) : attn_place<F::kRow>(mr + 8 * m2, m1));
 
     do {
       // ---- one segment
       const int head = cw.hb / a.blocks, q0 = (cw.hb - head * a.blocks) * kQ, qn = min(kQ, a.group - q0);
       uint32_t qf[NT][DP / 16][2];
+      float sc[NT][2];                                        // scores in powers of two per unit of the product, by query column
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int nt = 0; nt < NT; ++nt) {
+        const int q = nt * 8 + g;
+        const uint16_t* src = a.Q + cw.seq * a.q_stride + (long long)(head * a.group + q0 + q) * a.c.dim;
 #pragma unroll
         for (int k = 0; k < DP / 16; ++k) {
-          const int dim = I8 ? (k / 4) * 64 + t * 16 + (k % 4) * 4 : (k / 2) * 32 + t * 8 + (k % 2) * 4, q = nt * 8 + g;
-          uint2 v = make_uint2(0, 0);
-          if (q < qn && dim < a.c.dim)
-            v = __ldcg(reinterpret_cast<const uint2*>(a.Q + cw.seq * a.q_stride + (long long)(head * a.group + q0 + q) * a.c.dim + dim));
-          qf[nt][k][0] = v.x;
-          qf[nt][k][1] = v.y;
+          qf[nt][k][0] = qf[nt][k][1] = 0;
+          if constexpr (I8) {                                 // a thread of the product holds four neighbouring codes
+            const int dim = k * 16 + t * 4;
+            if (q < qn && dim < a.c.dim) {
+              const uint2 v = __ldcg(reinterpret_cast<const uint2*>(src + dim));
+              qf[nt][k][0] = v.x;
+              qf[nt][k][1] = v.y;
+            }
+          } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int dim = k * 16 + 8 * h + t * 2;
+              if (q < qn && dim < a.c.dim) qf[nt][k][h] = __ldcg(reinterpret_cast<const uint32_t*>(src + dim));
+            }
+          }
         }
-      float o[NT][DP / 16][4] = {}, m[NT][2], l[NT][2] = {};
+        sc[nt][0] = sc[nt][1] = a.scale_log2;
+        if constexpr (I8) {                                   // to fp16, the largest of the row just below 2^15
+          uint32_t top = 0;
+#pragma unroll
+          for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) top = max(top, max(qf[nt][k][i] << 16 & 0x7fff0000u, qf[nt][k][i] & 0x7fff0000u));
+          top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          const int up = top >= 0x7f800000u ? 0 : min(126, 127 + 14 - (int)(top >> 23));
+          const float f = __uint_as_float((uint32_t)(127 + up) << 23);
+#pragma unroll
+          for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) qf[nt][k][i] = pack_f16x2(bf16lo(qf[nt][k][i]) * f, bf16hi(qf[nt][k][i]) * f);
+          const float down = __uint_as_float((uint32_t)(127 - up) << 23) * a.scale_log2;
+          sc[nt][0] = __shfl_sync(0xffffffffu, down, 8 * t);
+          sc[nt][1] = __shfl_sync(0xffffffffu, down, 8 * t + 4);
+        }
+      }
+      // m: maximum of the scores so far, mu: what is taken off them (0 while there is no weight: every score is -infinity)
+      float o[NT][DP / 16][4] = {}, m[NT][2], mu[NT][2] = {}, l[NT][2] = {};
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) m[nt][0] = m[nt][1] = -INFINITY;
       const int seg_len = cw.len;
       for (int tile = cw.t0; tile < cw.t1; ++tile) {
         attn_copy_wait<F::kStages - 2>();
-        issue(ahead);                                          // into the place that this tile's predecessor has left
-        const uint32_t src = ring + stage * F::kStageBytes;
+        __syncwarp();                                          // every lane's copies are there, and the tile before has been read
+        issue(ahead);                                          // into the place that it has left
+        const uint32_t src = ring_at + stage * F::kStageBytes;
         // scores: rows g, g + 8 of the tile, query columns 2 t, 2 t + 1
         float s[NT][4] = {}, s2[NT][4] = {};
 #pragma unroll
-        for (int j = 0; j < F::kK; ++j) {
-          const uint4 ka = attn_lds128(src + (2 * j) * 512), kb = attn_lds128(src + (2 * j + 1) * 512);
-          const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+        for (int j = 0; j < F::kChunks / 2; ++j) {
+          uint32_t w[4];
+          ldmatrix4((src + k_mat) ^ (j << 5), w);
           if constexpr (I8) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t a0 = codes_lo(wa[i]), a1 = codes_lo(wb[i]), a2 = codes_hi(wa[i]), a3 = codes_hi(wb[i]);
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t xa = w[2 * h] ^ 0x80808080u, xb = w[2 * h + 1] ^ 0x80808080u;
+              const uint32_t a0 = codes_pair<0x4140>(xa), a1 = codes_pair<0x4140>(xb), a2 = codes_pair<0x4342>(xa), a3 = codes_pair<0x4342>(xb);
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) mma_bf16(i & 1 ? s2[nt] : s[nt], a0, a1, a2, a3, qf[nt][4 * j + i][0], qf[nt][4 * j + i][1]);
+              for (int nt = 0; nt < NT; ++nt) mma_f16(h ? s2[nt] : s[nt], a0, a1, a2, a3, qf[nt][2 * j + h][0], qf[nt][2 * j + h][1]);
             }
           } else {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt)
-                mma_bf16(i & 1 ? s2[nt] : s[nt], wa[2 * i], wb[2 * i], wa[2 * i + 1], wb[2 * i + 1], qf[nt][2 * j + i][0], qf[nt][2 * j + i][1]);
+            for (int nt = 0; nt < NT; ++nt) mma_bf16(j & 1 ? s2[nt] : s[nt], w[0], w[1], w[2], w[3], qf[nt][j][0], qf[nt][j][1]);
           }
         }
-        float fk[2] = {a.scale_log2, a.scale_log2}, fv[2] = {1.f, 1.f};
-        const int valid = seg_len - tile * kAttnTile;         // rows of the tile that the sequence holds
+        float gv[2] = {1.f, 1.f};
         if constexpr (I8) {
-          const uint4 gm = attn_lds128(src + (F::kSlots - 1) * 512);
-          fk[0] = __fdividef(a.scale_log2, __uint_as_float(gm.x)); fk[1] = __fdividef(a.scale_log2, __uint_as_float(gm.y));
-          fv[0] = __fdividef(1.f, __uint_as_float(gm.z)); fv[1] = __fdividef(1.f, __uint_as_float(gm.w));
+          const float* gm = reinterpret_cast<const float*>(smem + F::kGammaAt + warp * (F::kStages * F::kGammaBytes) + stage * F::kGammaBytes);
+          const float rk[2] = {attn_rcp(gm[g]), attn_rcp(gm[g + 8])};
+          gv[0] = gm[16 + g];
+          gv[1] = gm[24 + g];
+          const float lg[2] = {attn_log2(gv[0]), attn_log2(gv[1])};
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[nt][i] = (s[nt][i] + s2[nt][i]) * (rk[i >> 1] * sc[nt][i & 1]) - lg[i >> 1];
+        } else {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[nt][i] = (s[nt][i] + s2[nt][i]) * sc[nt][i & 1];
+        }
+        const int valid = seg_len - tile * kAttnTile;         // rows of the tile that the sequence holds
+        if (valid < kAttnTile) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (g + 8 * (i >> 1) >= valid) {
+              gv[i >> 1] = 0.f;
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) s[nt][i] = -INFINITY;
+            }
         }
         bool grew = false;
         float top[NT][2];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            s[nt][i] = (s[nt][i] + s2[nt][i]) * fk[i >> 1];
-            if (g + 8 * (i >> 1) >= valid) s[nt][i] = -INFINITY;
-          }
-#pragma unroll
-          for (int cidx = 0; cidx < 2; ++cidx) {
-            float v = fmaxf(s[nt][cidx], s[nt][cidx + 2]);
+          for (int c = 0; c < 2; ++c) {
+            float v = fmaxf(s[nt][c], s[nt][c + 2]);
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
-            top[nt][cidx] = fmaxf(v, m[nt][cidx]);
-            grew |= top[nt][cidx] > m[nt][cidx];
+            top[nt][c] = v;
+            grew |= v > m[nt][c];
           }
-        }
         if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int cidx = 0; cidx < 2; ++cidx) {
-              const float f = top[nt][cidx] > m[nt][cidx] ? exp2f(m[nt][cidx] - top[nt][cidx]) : 1.f;
-              m[nt][cidx] = top[nt][cidx];
-              l[nt][cidx] *= f;
+            for (int c = 0; c < 2; ++c) {
+              if (!(top[nt][c] > m[nt][c])) continue;
+              const float f = attn_exp2(m[nt][c] - top[nt][c]);
+              m[nt][c] = top[nt][c];
+              mu[nt][c] = I8 ? top[nt][c] - kWeightTop : top[nt][c];
+              l[nt][c] *= f;
 #pragma unroll
-              for (int i = 0; i < DP / 16; ++i) { o[nt][i][cidx] *= f; o[nt][i][cidx + 2] *= f; }
+              for (int i = 0; i < DP / 16; ++i) { o[nt][i][c] *= f; o[nt][i][c + 2] *= f; }
             }
         }
         uint32_t ph[NT][2], pl[NT][2];
@@ -320,167 +443,227 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
           float p[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float mm = m[nt][i & 1] == -INFINITY ? 0.f : m[nt][i & 1];      // no weight so far: every score is -infinity
-            p[i] = exp2f(s[nt][i] - mm);
-            l[nt][i & 1] += p[i];
-            if (I8) p[i] = g + 8 * (i >> 1) < valid ? p[i] * fv[i >> 1] : 0.f;
+            p[i] = attn_exp2(s[nt][i] - mu[nt][i & 1]);
+            l[nt][i & 1] = I8 ? fmaf(p[i], gv[i >> 1], l[nt][i & 1]) : l[nt][i & 1] + p[i];
           }
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const uint32_t hi = pack_bf16x2(p[2 * h], p[2 * h + 1]);
-            const uint32_t low = pack_bf16x2(p[2 * h] - bf16lo(hi), p[2 * h + 1] - bf16hi(hi));
-            ph[nt][h] = transpose8x8(hi);
-            pl[nt][h] = transpose8x8(low);
+            if constexpr (I8) {
+              ph[nt][h] = transpose8x8(pack_f16x2(p[2 * h], p[2 * h + 1]));
+            } else {
+              const uint32_t hi = pack_bf16x2(p[2 * h], p[2 * h + 1]);
+              ph[nt][h] = transpose8x8(hi);
+              pl[nt][h] = transpose8x8(pack_bf16x2(p[2 * h] - bf16lo(hi), p[2 * h + 1] - bf16hi(hi)));
+            }
           }
         }
 #pragma unroll
-        for (int j = 0; j < F::kV; ++j) {
-          uint4 r[4];
-#pragma unroll
-          for (int h = 0; h < 4; ++h) r[h] = attn_lds128(src + (2 * F::kK + 4 * j + h) * 512);
-          const uint32_t w0[4] = {r[0].x, r[0].y, r[0].z, r[0].w}, w1[4] = {r[1].x, r[1].y, r[1].z, r[1].w};
-          const uint32_t w2[4] = {r[2].x, r[2].y, r[2].z, r[2].w}, w3[4] = {r[3].x, r[3].y, r[3].z, r[3].w};
-          auto product = [&](int mt, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              mma_bf16(o[nt][mt], a0, a1, a2, a3, ph[nt][0], ph[nt][1]);
-              mma_bf16(o[nt][mt], a0, a1, a2, a3, pl[nt][0], pl[nt][1]);
-            }
-          };
+        for (int j = 0; j < F::kChunks / 2; ++j) {
+          uint32_t w[4];
+          ldmatrix4_trans((src + v_mat) ^ (j << 5), w);
           if constexpr (I8) {
 #pragma unroll
-            for (int i = 0; i < F::kVBytes / 4; ++i) {
-              const uint32_t x01 = __byte_perm(w0[i], w1[i], 0x5140), x23 = __byte_perm(w2[i], w3[i], 0x5140);
-              const uint32_t y01 = __byte_perm(w0[i], w1[i], 0x7362), y23 = __byte_perm(w2[i], w3[i], 0x7362);
-              product(j * 8 + 2 * i, codes_lo(x01), codes_hi(x01), codes_lo(x23), codes_hi(x23));
-              product(j * 8 + 2 * i + 1, codes_lo(y01), codes_hi(y01), codes_lo(y23), codes_hi(y23));
+            for (int h = 0; h < 2; ++h) {                      // an m-tile: row g the even dim of the g-th pair of a piece, row g + 8 the odd one
+              const uint32_t x0 = w[2 * h] ^ 0x80808080u, x1 = w[2 * h + 1] ^ 0x80808080u;
+              const uint32_t a0 = codes_pair<0x4240>(x0), a1 = codes_pair<0x4341>(x0), a2 = codes_pair<0x4240>(x1), a3 = codes_pair<0x4341>(x1);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][2 * j + h], a0, a1, a2, a3, ph[nt][0], ph[nt][1]);
             }
           } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              product(j * 4 + i, __byte_perm(w0[i], w1[i], 0x5410), __byte_perm(w0[i], w1[i], 0x7632), __byte_perm(w2[i], w3[i], 0x5410),
-                      __byte_perm(w2[i], w3[i], 0x7632));
+            for (int nt = 0; nt < NT; ++nt) {
+              mma_bf16(o[nt][j], w[0], w[1], w[2], w[3], ph[nt][0], ph[nt][1]);
+              mma_bf16(o[nt][j], w[0], w[1], w[2], w[3], pl[nt][0], pl[nt][1]);
+            }
           }
         }
         stage = stage + 1 == F::kStages ? 0 : stage + 1;
         ahead = ahead + 1 == F::kStages ? 0 : ahead + 1;
       }
-      // ---- the segment's sums
+      // ---- the segment's sums: out, or left for the join -- a warp's last piece in its ring, whose copies have all landed and been
+      // read, one before it in global memory
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int cidx = 0; cidx < 2; ++cidx)
+        for (int c = 0; c < 2; ++c)
 #pragma unroll
-          for (int d = 4; d < 32; d <<= 1) l[nt][cidx] += __shfl_xor_sync(0xffffffffu, l[nt][cidx], d);
-      const bool whole = cw.t0 == 0 && cw.t1 == cw.tiles;
-      const int slot = 2 * team + (cw.t0 == 0 ? 1 : 0);
-      constexpr int kRun = 2 * F::kVBytes / (I8 ? 2 : 4);      // neighbouring dims of a lane in a piece: 8 (bf16, short int8 rows) or 16
+          for (int d = 4; d < 32; d <<= 1) l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], d);
+      const bool whole = cw.t0 == 0 && cw.t1 == cw.tiles, last = cw.left == 0;
+      float* const part = last ? reinterpret_cast<float*>(ring) : a.warp_part + (long long)(cta * kWarps + warp) * kQ * DP;
+      const int at = 2 * warp + (last ? 1 : 0);
+      if (!whole) {
+        if (last) { attn_copy_wait<0>(); __syncwarp(); }
+        if (lane == 0) pieces[at] = AttnPiece{cw.seq * per_seq + cw.hb, cw.seq, cw.hb, cw.t0 == 0, cw.t1 == cw.tiles};
+      }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int cidx = 0; cidx < 2; ++cidx) {
-          const int q = nt * 8 + 2 * t + cidx;
+        for (int c = 0; c < 2; ++c) {
+          const int q = nt * 8 + 2 * t + c;
           if (q >= qn) continue;
-          const float inv = l[nt][cidx] == 0.f ? 0.f : 1.f / l[nt][cidx];
+          const float inv = attn_inv(l[nt][c]);
           const long long qrow = (long long)cw.seq * a.q_heads + head * a.group + q0 + q;
 #pragma unroll
-          for (int j = 0; j < F::kV; ++j)
-#pragma unroll
-            for (int i = 0; i < kRun / 2; i += 2) {            // four neighbouring dims at a time: head_dim is a multiple of 4
-              const int mt = j * (kRun / 2) + i, dim = j * 8 * kRun + g * kRun + 2 * i;
-              if (dim >= a.c.dim) continue;
-              const float v0 = o[nt][mt][cidx], v1 = o[nt][mt][cidx + 2], v2 = o[nt][mt + 1][cidx], v3 = o[nt][mt + 1][cidx + 2];
-              if (whole) *reinterpret_cast<uint2*>(a.O + qrow * a.c.dim + dim) = make_uint2(pack_bf16x2(v0 * inv, v1 * inv), pack_bf16x2(v2 * inv, v3 * inv));
-              else *reinterpret_cast<float4*>(a.part + ((long long)slot * kQ + q) * DP + dim) = make_float4(v0, v1, v2, v3);
+          for (int i = 0; i < DP / 16; ++i) {
+            const int dim = 16 * i + (I8 ? 2 * g : g), dim2 = I8 ? dim + 1 : dim + 8;      // of rows g and g + 8
+            if (!whole) {
+              part[q * DP + dim] = o[nt][i][c];
+              part[q * DP + dim2] = o[nt][i][c + 2];
+            } else {
+              const uint32_t two = pack_bf16x2(o[nt][i][c] * inv, o[nt][i][c + 2] * inv);
+              uint16_t* out = a.O + qrow * a.c.dim;
+              if (I8) {
+                if (dim < a.c.dim) *reinterpret_cast<uint32_t*>(out + dim) = two;
+              } else {
+                if (dim < a.c.dim) out[dim] = (uint16_t)two;
+                if (dim2 < a.c.dim) out[dim2] = (uint16_t)(two >> 16);
+              }
             }
+          }
           if (g == 0) {
-            if (!whole) a.part_ml[(long long)slot * kQ + q] = make_float2(m[nt][cidx], l[nt][cidx]);
-            else if (a.lse) a.lse[qrow] = l[nt][cidx] == 0.f ? -INFINITY : (m[nt][cidx] + log2f(l[nt][cidx])) * kLn2;
+            if (!whole) piece_ml[at][q] = make_float2(l[nt][c] == 0.f ? -INFINITY : mu[nt][c], l[nt][c]);
+            else if (a.lse) a.lse[qrow] = attn_lse(mu[nt][c], l[nt][c]);
           }
         }
-      if (cw.t0 == 0 && lane == 0) {                           // the holder of an item's beginning says what there is to join
-        const int item = cw.seq * per_seq + cw.hb;
-        int pieces = 0;
-        if (!whole) {
-          const long long last = r1 - cw.left + (cw.tiles - cw.t1) - 1;     // the item's last tile; its team is the last t with t tiles_all / used <= it
-          pieces = (int)(((last + 1) * used - 1) / tiles_all) - team + 1;
-        }
-        if (a.head_by_item || !whole) a.head[a.head_by_item ? item : team] = make_int4(slot, pieces, item, 0);
-        headed |= !whole;
-      }
-    } while (cw.next(a, per_seq));
+    } while (cw.next(a, lens, per_seq));
+    attn_copy_wait<0>();
   }
-  if (!a.head_by_item && lane == 0 && !headed) a.head[team] = make_int4(0, 0, 0, 0);
   // ---- sequences without a position: zeros, or, of negative length, left as they were
-  for (int s = team; s < n; s += a.teams) {
-    const int len = attn_len(a, s);
-    if (len > 0) continue;
-    if (len == 0) {
-      for (int i = lane * 4; i < a.q_heads * a.c.dim; i += 128) *reinterpret_cast<uint2*>(a.O + (long long)s * a.q_heads * a.c.dim + i) = make_uint2(0, 0);
-      if (a.lse) for (int i = lane; i < a.q_heads; i += 32) a.lse[(long long)s * a.q_heads + i] = -INFINITY;
-    }
-    if (a.head_by_item) for (int i = lane; i < per_seq; i += 32) a.head[s * per_seq + i] = make_int4(0, 0, 0, 0);
+  for (int s = cta * kWarps + warp; s < n; s += gridDim.x * kWarps) {
+    if (attn_len(a, lens, s) != 0) continue;
+    for (int i = lane * 4; i < a.q_heads * a.c.dim; i += 128) *reinterpret_cast<uint2*>(a.O + (long long)s * a.q_heads * a.c.dim + i) = make_uint2(0, 0);
+    if (a.lse) for (int i = lane; i < a.q_heads; i += 32) a.lse[(long long)s * a.q_heads + i] = -INFINITY;
   }
-}
-
-// ---------------------------------------------------------------------------
-// k_attn_join: the pieces of an item that several warps worked on, one block per (entry of head, query head), added in the order
-// of their positions.  Slots of the pieces: the first one, then the even slots of the teams behind it.
-// ---------------------------------------------------------------------------
-constexpr int kJoinThreads = 256;
-__global__ void __launch_bounds__(kJoinThreads) k_attn_join(const __grid_constant__ AttnArgs a, int width, int cols, int entries) {
-  constexpr int kWarps = kJoinThreads / 32;
-  __shared__ float tops[kWarps], sums[kWarps], out[kWarps][256];
-  pdl_launch_dependents();
-  pdl_wait();
-  const int q = blockIdx.y, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, per_seq = a.c.heads * a.blocks;
-  for (int entry = blockIdx.x; entry < entries; entry += gridDim.x) {
-    const int4 e = __ldcg(a.head + entry);
-    const int pieces = e.y, item = e.z;
-    if (pieces == 0) continue;
-    const int seq = item / per_seq, hb = item - seq * per_seq, head = hb / a.blocks, q0 = (hb - head * a.blocks) * cols;
-    if (q0 + q >= a.group) continue;
-    auto slot = [&](int i) { return (long long)(i == 0 ? e.x : (e.x & ~1) + 2 * i) * cols + q; };
-    // a warp takes every eighth piece, a lane four neighbouring dims and the four 128 behind them
-    float m = -INFINITY;
-    for (int i = tid; i < pieces; i += kJoinThreads) m = fmaxf(m, __ldcg(&a.part_ml[slot(i)]).x);
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    if (lane == 0) tops[warp] = m;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) m = fmaxf(m, tops[w]);
-    if (m == -INFINITY) m = 0.f;                    // no weight anywhere
-    float4 acc[2] = {make_float4(0, 0, 0, 0), make_float4(0, 0, 0, 0)};
-    float l = 0.f;
-    for (int i = warp; i < pieces; i += kWarps) {
-      const float2 ml = __ldcg(&a.part_ml[slot(i)]);
-      const float f = exp2f(ml.x - m);
-      l += ml.y * f;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int dim = lane * 4 + 128 * h;
-        if (dim >= a.c.dim) continue;
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(a.part + slot(i) * width + dim));
-        acc[h].x += v.x * f; acc[h].y += v.y * f; acc[h].z += v.z * f; acc[h].w += v.w * f;
+  if (c0 >= c1) return;
+  __syncthreads();
+  // ---- join in the CTA: runs of pieces of the same item, a unit of four dims of a query head per thread.  Runs are found by every
+  // warp for itself: lane e looks at piece e (there are at most 32).
+  const int item_e = lane < 2 * kWarps ? pieces[lane].item : -1;
+  const uint32_t have = __ballot_sync(0xffffffffu, item_e >= 0);
+  const uint32_t below = have & ((1u << lane) - 1u);
+  const int prev = __shfl_sync(0xffffffffu, item_e, below ? 31 - __clz(below) : 0);
+  uint32_t starts = __ballot_sync(0xffffffffu, item_e >= 0 && (below == 0 || prev != item_e));
+  int tail0 = 0, tail1 = 0;                                    // pieces of the items that go on before, behind this CTA (they are joined by the last)
+  AttnPiece run0{}, run1{};
+  constexpr int kUnits = kQ * DP / 4;
+  for (int run = 0; starts; ++run) {
+    const int e0 = __ffs(starts) - 1;
+    starts &= starts - 1;
+    const uint32_t mask = have & ~((1u << e0) - 1u) & (starts ? (1u << (__ffs(starts) - 1)) - 1u : 0xffffffffu);
+    const int e1 = 31 - __clz(mask);
+    const AttnPiece pc = pieces[e0];
+    const bool from = pc.whole_from, to = pieces[e1].whole_to;
+    const int head = pc.hb / a.blocks, q0 = (pc.hb - head * a.blocks) * kQ, qn = min(kQ, a.group - q0);
+    for (int u = tid; u < kUnits; u += kThreads) {
+      const int q = u / (DP / 4), dim = u % (DP / 4) * 4;
+      if (q >= qn || dim >= a.c.dim) continue;
+      float top = -INFINITY;
+      for (uint32_t left = mask; left; left &= left - 1) top = fmaxf(top, piece_ml[__ffs(left) - 1][q].x);
+      const float off = top == -INFINITY ? 0.f : top;
+      float4 acc = make_float4(0, 0, 0, 0);
+      float l = 0.f;
+      for (uint32_t left = mask; left; left &= left - 1) {
+        const int e = __ffs(left) - 1;
+        const float2 ml = piece_ml[e][q];
+        const float f = attn_exp2(ml.x - off);
+        l += ml.y * f;
+        const float4 v = e & 1 ? *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(smem + (e >> 1) * (F::kStages * F::kStageBytes)) + q * DP + dim)
+                               : __ldcg(reinterpret_cast<const float4*>(a.warp_part + ((long long)(cta * kWarps + (e >> 1)) * kQ + q) * DP + dim));
+        acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
+      }
+      if (from && to) {
+        const long long qrow = (long long)pc.seq * a.q_heads + head * a.group + q0 + q;
+        attn_store(a, qrow, dim, acc.x, acc.y, acc.z, acc.w, attn_inv(l));
+        if (dim == 0 && a.lse) a.lse[qrow] = attn_lse(top, l);
+      } else {
+        const long long slot = 2 * cta + (from ? 1 : 0);
+        __stcg(reinterpret_cast<float4*>(a.cta_part + (slot * kQ + q) * DP + dim), acc);
+        if (dim == 0) __stcg(a.cta_ml + slot * kQ + q, make_float2(top, l));
       }
     }
-#pragma unroll
-    for (int h = 0; h < 2; ++h) *reinterpret_cast<float4*>(&out[warp][lane * 4 + 128 * h]) = acc[h];
-    if (lane == 0) sums[warp] = l;
-    __syncthreads();
-    l = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) l += sums[w];
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const long long qrow = (long long)seq * a.q_heads + head * a.group + q0 + q;
-    if (tid < a.c.dim) {
-      float v = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) v += out[w][tid];
-      a.O[qrow * a.c.dim + tid] = (uint16_t)(pack_bf16x2(v * inv, 0.f) & 0xffffu);
+    if (!(from && to)) {                                       // goes on before this CTA, or behind it, or both
+      if (!from) { run0 = pc; tail0 = 1; } else { run1 = pc; tail1 = 1; }
     }
-    if (tid == 0 && a.lse) a.lse[qrow] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+  }
+  if (!(tail0 | tail1)) return;
+  // ---- join between CTAs: by the last to arrive.  The CTA where the item begins keeps the count.
+  for (int side = 0; side < 2; ++side) {
+    if (!(side ? tail1 : tail0)) continue;
+    const AttnPiece pc = side ? run1 : run0;
+    // the item's tiles, and the CTAs that hold the first and the last of them: CTA c holds x when c tiles_all / used <= x, c the largest such
+    long long base = 0;
+    {
+      const int th = pc.seq / per;
+      base = sums[th];
+      for (int s = th * per; s < pc.seq; ++s) base += (max(0, attn_len(a, lens, s)) + kAttnTile - 1) / kAttnTile;
+    }
+    const int tiles = (attn_len(a, lens, pc.seq) + kAttnTile - 1) / kAttnTile;
+    const long long x0 = base * per_seq + (long long)pc.hb * tiles, x1 = x0 + tiles - 1;
+    const int f0 = (int)(((x0 + 1) * used - 1) / tiles_all), f1 = (int)(((x1 + 1) * used - 1) / tiles_all), np = f1 - f0 + 1;
+    __threadfence();
+    __syncthreads();                                           // this CTA's piece is in memory
+    if (tid == 0) {
+      unsigned long long* const word = a.arrived + f0;
+      unsigned long long seen = *reinterpret_cast<volatile unsigned long long*>(word), put;
+      int count;
+      for (;;) {                                               // ends: every failure is another CTA's success, and there are np of those
+        count = (seen >> 16) == (a.call >> 16) ? (int)(seen & 0xffff) + 1 : 1;
+        put = count == np ? 0 : a.call | (unsigned)count;
+        const unsigned long long got = atomicCAS(word, seen, put);
+        if (got == seen) break;
+        seen = got;
+      }
+      __threadfence();
+      arrived_last = count == np;
+    }
+    __syncthreads();
+    if (!arrived_last) continue;
+    const int head = pc.hb / a.blocks, q0 = (pc.hb - head * a.blocks) * kQ, qn = min(kQ, a.group - q0);
+    // weights of the pieces into shared memory (the rings are free), then the units, split over the pieces where threads are left
+    float* const fac = reinterpret_cast<float*>(smem);         // [np][kQ]
+    float* const tops = fac + np * kQ;                         // [kQ] top, [kQ] l
+    auto slot_of = [&](int i) { return (long long)(2 * (f0 + i) + (i == 0 ? 1 : 0)); };
+    for (int q = warp; q < qn; q += kWarps) {
+      float top = -INFINITY, l = 0.f;
+      for (int i = lane; i < np; i += 32) top = fmaxf(top, __ldcg(&a.cta_ml[slot_of(i) * kQ + q]).x);
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+      const float off = top == -INFINITY ? 0.f : top;
+      for (int i = lane; i < np; i += 32) {
+        const float2 ml = __ldcg(&a.cta_ml[slot_of(i) * kQ + q]);
+        const float f = attn_exp2(ml.x - off);
+        fac[i * kQ + q] = f;
+        l += ml.y * f;
+      }
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+      if (lane == 0) { tops[q] = top; tops[kQ + q] = l; }
+    }
+    __syncthreads();
+    const int units = qn * (DP / 4);
+    int split = 1;                                             // threads that share a unit's pieces: a power of two, in one warp
+    while (split < 32 && units * split * 2 <= kThreads && split < np) split *= 2;
+    for (int u0 = 0; u0 < units; u0 += kThreads / split) {
+      const int u = u0 + tid / split, part = tid % split, q = u / (DP / 4), dim = u % (DP / 4) * 4;
+      float4 acc = make_float4(0, 0, 0, 0);
+      if (u < units && dim < a.c.dim) {
+#pragma unroll 4
+        for (int i = part; i < np; i += split) {
+          const float4 v = __ldcg(reinterpret_cast<const float4*>(a.cta_part + (slot_of(i) * kQ + q) * DP + dim));
+          const float f = fac[i * kQ + q];
+          acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
+        }
+      }
+      for (int d = 1; d < split; d <<= 1) {
+        acc.x += __shfl_xor_sync(0xffffffffu, acc.x, d); acc.y += __shfl_xor_sync(0xffffffffu, acc.y, d);
+        acc.z += __shfl_xor_sync(0xffffffffu, acc.z, d); acc.w += __shfl_xor_sync(0xffffffffu, acc.w, d);
+      }
+      if (u < units && dim < a.c.dim && part == 0) {
+        const long long qrow = (long long)pc.seq * a.q_heads + head * a.group + q0 + q;
+        attn_store(a, qrow, dim, acc.x, acc.y, acc.z, acc.w, attn_inv(tops[kQ + q]));
+        if (dim == 0 && a.lse) a.lse[qrow] = attn_lse(tops[q], tops[kQ + q]);
+      }
+    }
     __syncthreads();
   }
 }
@@ -488,41 +671,54 @@ __global__ void __launch_bounds__(kJoinThreads) k_attn_join(const __grid_constan
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
-struct AttnPlan { int dp, nt, warps, teams, blocks; long long items, heads; };
-static AttnPlan attn_plan(const KvCache& c, int q_heads) {
-  AttnPlan p{};
-  p.dp = c.dim <= 64 ? 64 : c.dim <= 128 ? 128 : 256;
-  const int group = q_heads / c.heads;
-  p.nt = group > 8 && p.dp < 256 ? 2 : 1;         // head_dim above 128: the accumulators of two blocks do not fit
-  p.blocks = (group + 8 * p.nt - 1) / (8 * p.nt);
-  p.warps = p.dp == 256 ? 4 : 8;
-  p.teams = p.warps * sm_count();
-  p.items = (long long)c.num_seqs * c.heads * p.blocks;
-  p.heads = std::min<long long>(p.items, p.teams);
-  return p;
-}
-static size_t attn_carve(const AttnPlan& p, void* base, AttnArgs* a) {
-  size_t off = 0;
-  auto take = [&](size_t bytes) { uint8_t* q = static_cast<uint8_t*>(base) + off; off += (bytes + 255) / 256 * 256; return q; };
-  uint8_t* part = take((size_t)2 * p.teams * 8 * p.nt * p.dp * 4);
-  uint8_t* ml = take((size_t)2 * p.teams * 8 * p.nt * 8);
-  uint8_t* head = take((size_t)p.heads * 16);
-  if (a) { a->part = reinterpret_cast<float*>(part); a->part_ml = reinterpret_cast<float2*>(ml); a->head = reinterpret_cast<int4*>(head); }
-  return off;
-}
-size_t attn_workspace_bytes(const KvCache& c, int q_heads) { return attn_carve(attn_plan(c, q_heads), nullptr, nullptr); }
-
 using AttnKernel = void (*)(AttnArgs);
-struct AttnChoice { AttnKernel kernel; int smem; };
+struct AttnChoice { AttnKernel kernel; int smem, warps; };
 template <int DP, int NT>
 static AttnChoice attn_choice(bool i8) {
-  return i8 ? AttnChoice{k_attn_decode<DP, NT, true>, AttnForm<DP, NT, true>::kSmem} : AttnChoice{k_attn_decode<DP, NT, false>, AttnForm<DP, NT, false>::kSmem};
+  return i8 ? AttnChoice{k_attn_decode<DP, NT, true>, AttnForm<DP, NT, true>::kSmem, AttnForm<DP, NT, true>::kWarps}
+            : AttnChoice{k_attn_decode<DP, NT, false>, AttnForm<DP, NT, false>::kSmem, AttnForm<DP, NT, false>::kWarps};
 }
 static AttnChoice attn_choice(int dp, int nt, bool i8) {
   if (dp == 64) return nt == 1 ? attn_choice<64, 1>(i8) : attn_choice<64, 2>(i8);
   if (dp == 128) return nt == 1 ? attn_choice<128, 1>(i8) : attn_choice<128, 2>(i8);
   return attn_choice<256, 1>(i8);
 }
+struct AttnPlan { AttnChoice choice; int dp, nt, blocks; };
+static AttnPlan attn_plan(const KvCache& c, int q_heads) {
+  AttnPlan p{};
+  p.dp = c.dim <= 64 ? 64 : c.dim <= 128 ? 128 : 256;
+  const int group = q_heads / c.heads;
+  p.nt = group > 8 && p.dp < 256 ? 2 : 1;         // head_dim above 128: the accumulators of two blocks do not fit
+  p.blocks = (group + 8 * p.nt - 1) / (8 * p.nt);
+  p.choice = attn_choice(p.dp, p.nt, c.format == PQ_KV_INT8);
+  return p;
+}
+static size_t attn_carve(const AttnPlan& p, void* base, AttnArgs* a) {
+  size_t off = 0;
+  const size_t ctas = sm_count(), piece = (size_t)8 * p.nt * p.dp;
+  auto take = [&](size_t bytes) { uint8_t* q = static_cast<uint8_t*>(base) + off; off += (bytes + 255) / 256 * 256; return q; };
+  uint8_t* warp_part = take(ctas * p.choice.warps * piece * 4);
+  uint8_t* cta_part = take(2 * ctas * piece * 4);
+  uint8_t* ml = take(2 * ctas * 8 * p.nt * 8);
+  uint8_t* arrived = take(ctas * 8);
+  if (a) {
+    a->warp_part = reinterpret_cast<float*>(warp_part); a->cta_part = reinterpret_cast<float*>(cta_part);
+    a->cta_ml = reinterpret_cast<float2*>(ml); a->arrived = reinterpret_cast<unsigned long long*>(arrived);
+  }
+  return off;
+}
+size_t attn_workspace_bytes(const KvCache& c, int q_heads) { return attn_carve(attn_plan(c, q_heads), nullptr, nullptr); }
+
+// Numbers of launches, so that a count left in a workspace by something else is not taken for one of this launch: from a start that the
+// clock and this library's address spread over 48 bits.  A launch in a graph keeps its number; the last to arrive clears the count.
+static unsigned long long attn_call_number() {
+  static std::atomic<unsigned long long> next{(unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count() * 0x9E3779B97F4A7C15ull ^
+                                              reinterpret_cast<uintptr_t>(&attn_call_number)};
+  unsigned long long v;
+  do { v = next.fetch_add(1, std::memory_order_relaxed) << 16; } while (v == 0);
+  return v;
+}
+
 // The opt-in limits, once per device
 static cudaError_t attn_limits() {
   constexpr int kMaxDevices = 64;
@@ -550,18 +746,11 @@ cudaError_t launch_attn_decode(const KvCache& c, int q_heads, const uint16_t* Q,
   AttnArgs a{};
   a.c = c; a.Q = Q; a.q_stride = q_stride; a.lens = lens; a.O = O; a.lse = lse;
   a.scale_log2 = scale * kLog2e;
-  a.q_heads = q_heads; a.group = q_heads / c.heads; a.blocks = p.blocks; a.teams = p.teams;
-  a.head_by_item = p.items <= p.teams;
+  a.q_heads = q_heads; a.group = q_heads / c.heads; a.blocks = p.blocks;
+  a.call = attn_call_number();
   attn_carve(p, ws, &a);
-  const AttnChoice ch = attn_choice(p.dp, p.nt, c.format == PQ_KV_INT8);
-  {
-    LaunchScope ls(KID_ATTN_DECODE, st);
-    if (const cudaError_t e = launch_pdl(ch.kernel, p.teams / p.warps, p.warps * 32, ch.smem, st, a)) return e;
-  }
-  LaunchScope ls(KID_ATTN_JOIN, st);
-  const int rows = std::min(a.group, 8 * p.nt);
-  return launch_pdl(k_attn_join, dim3((unsigned)std::min<long long>(p.heads, std::max(1, 4 * sm_count() / rows)), (unsigned)rows), kJoinThreads, 0, st, a,
-                    p.dp, 8 * p.nt, (int)p.heads);
+  LaunchScope ls(KID_ATTN_DECODE, st);
+  return launch_pdl(p.choice.kernel, sm_count(), p.choice.warps * 32, p.choice.smem, st, a);
 }
 
 }  // namespace pq

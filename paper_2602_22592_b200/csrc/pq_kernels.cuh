@@ -17,7 +17,7 @@ constexpr float kActAmaxFloor = 1e-5f;     // all-zero row guard
 enum KernelId : int {
   KID_PACK_SUMS = 0, KID_BINARIZE_PACK, KID_ROUTER, KID_ROUTE_SCAN, KID_ACT_QUANT, KID_HP_UP, KID_FWD, KID_SCATTER_ROWS,
   KID_SCALED_SIGN, KID_BWD_DW = 12, KID_SUM_PARTIALS = 16, KID_SUM_SCALAR, KID_DEBUG, KID_DECODE_PREP, KID_DECODE_MAIN,
-  KID_DECODE_PACK = 23, KID_DECODE_STREAM, KID_KV_APPEND, KID_KV_READ, KID_ATTN_DECODE, KID_ATTN_JOIN, KID_NORM_FWD, KID_NORM_BWD, KID_NORM_SUMS,
+  KID_DECODE_PACK = 23, KID_DECODE_STREAM, KID_KV_APPEND, KID_KV_READ, KID_ATTN_DECODE, KID_NORM_FWD, KID_NORM_BWD, KID_NORM_SUMS,
   KID_COUNT
 };
 struct ProfileSlot { cudaEvent_t start, stop; };

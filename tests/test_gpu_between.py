@@ -3,8 +3,9 @@ the 64-bit forms of oracle/between_oracle.py.
 
 Tolerances count roundings.  bf16 outputs: half a step, 2^-8 of the value.  Sums of n fp32 terms: n 2^-24 of the sum of the
 terms' sizes.  Attention: a score's error d (a dot product of head_dim terms, its scale and gamma) moves a weight by the factor
-e^d, and the weights enter the second product as two bf16 numbers (2^-16), so that an output moves by at most
-(2 d + 2^-16 + n 2^-24) sum |p v| / sum p.
+e^d, and the weights p enter the second product as two bf16 numbers (bf16 cache: w = 2^-16 of p) or one fp16 number (int8 cache: half a
+step, w = 2^-11 of p), while the sum that divides is of the unrounded ones.  sum (1 + a_j) p_j v_j with |a_j| <= w differs from sum
+p_j v_j by at most w sum |p_j v_j|, so that an output moves by at most (2 d + w + n 2^-24) sum |p v| / sum p.
 """
 import numpy as np
 import pytest
@@ -251,13 +252,14 @@ def test_places_that_do_not_exist_are_reported_and_nothing_is_touched():
 
 
 # --------------------------------------------------------------------------- attention
-def close_attention(O, lse, q, rows, scale):
+def close_attention(O, lse, q, rows, scale, int8=False):
     heads, dim = q.shape[1:]
+    w = 2.0 ** -11 if int8 else 2.0 ** -16
     O = f64(O).reshape(len(rows), heads, dim)
     for s, (k, v) in enumerate(rows):
         want, wl, spread, big = B.attend(q[s], k, v, scale)
         d = (dim + 8) * 2.0 ** -23 * big[:, None]
-        tol = HALF * np.abs(want) + (2 * d + 2.0 ** -16 + len(k) * 2.0 ** -24) * spread + 1e-30
+        tol = HALF * np.abs(want) + (2 * d + w + len(k) * 2.0 ** -24) * spread + 1e-30
         err = np.abs(O[s] - want)
         assert (err <= tol).all(), (s, len(k), float((err / tol).max()))
         if lse is not None:
@@ -291,7 +293,7 @@ def test_attention(heads, group, dim, page, lens, int8):
     pqb.pq_attn_decode(C.c, bf(q).view(n, -1), lt, scale, O, lse, ws)
     torch.cuda.synchronize()
     check_status()
-    close_attention(O, lse, q, rows, scale)
+    close_attention(O, lse, q, rows, scale, int8)
     assert guards_whole(raw) and guards_whole(raw_l) and guards_whole(ws_raw)
     # rows apart, no lse, a workspace full of NaN: the same bits
     wide = torch.full((n, H * dim + 12), float("nan"), dtype=torch.bfloat16, device=DEV)
@@ -339,7 +341,7 @@ def test_attention_of_many_sequences(n, heads, group, dim, most, int8):
     ws = torch.full((pqb.pq_attn_workspace_bytes(C.c, heads * group),), 255, dtype=torch.uint8, device=DEV)
     pqb.pq_attn_decode(C.c, bf(q).view(n, -1), torch.tensor(lens, dtype=torch.int32, device=DEV), 0.2, O, lse, ws)
     check_status()
-    close_attention(O, lse, q, rows, 0.2)
+    close_attention(O, lse, q, rows, 0.2, int8)
 
 
 @pytest.mark.parametrize("int8,group", [(False, 1), (True, 4), (False, 16)])
@@ -353,7 +355,7 @@ def test_attention_over_one_long_sequence(int8, group):
     ws = torch.empty(pqb.pq_attn_workspace_bytes(C.c, group), dtype=torch.uint8, device=DEV)
     pqb.pq_attn_decode(C.c, bf(q).view(1, -1), torch.tensor(lens, dtype=torch.int32, device=DEV), 128 ** -0.5, O, lse, ws)
     check_status()
-    close_attention(O, lse, q, rows, 128 ** -0.5)
+    close_attention(O, lse, q, rows, 128 ** -0.5, int8)
 
 
 def test_attention_with_extreme_scores():
@@ -447,7 +449,7 @@ def test_steps_replayed_from_graphs_and_on_another_stream():
         torch.cuda.synchronize()
         check_status()
         for st in sets:
-            close_attention(st["O"], None, st["want_q"], st["rows"], 0.125)
+            close_attention(st["O"], None, st["want_q"], st["rows"], 0.125, True)
             st["lens"] += 1
             st["pos"] += 1
     torch.cuda.synchronize()
