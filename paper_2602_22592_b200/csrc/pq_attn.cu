@@ -116,6 +116,7 @@ struct AttnArgs {
   unsigned long long call;   // a number of this launch, above 16 bits: what the workspace held before is recognised by its absence
 };
 
+constexpr int kFewPieces = 4;
 constexpr int kAttnLens = 1024;      // lengths kept in shared memory
 
 __device__ __forceinline__ int attn_len(const AttnArgs& a, const int* lens, int seq) {
@@ -141,6 +142,18 @@ struct AttnWalk {
   }
 };
 
+// Equal shares of all tiles: the first `more` CTAs take one tile more than the others
+struct AttnShares {
+  bool by_chunk;
+  int used, more;
+  long long each;
+  __device__ long long begin(int cta) const { return cta * each + min(cta, more); }
+  __device__ int holder(long long tile) const {               // the CTA whose share it is in
+    const long long cut = (each + 1) * more;
+    return (int)(tile < cut ? tile / (each + 1) : more + (tile - cut) / each);
+  }
+};
+
 // One piece of a cut item: what a warp leaves for the CTA's join
 struct AttnPiece {
   int item;                  // -1: none
@@ -156,21 +169,23 @@ __device__ __forceinline__ float attn_lse(float m, float l) { return l == 0.f ? 
 template <int DP, int NT, bool I8>
 __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_decode(const __grid_constant__ AttnArgs a) {
   using F = AttnForm<DP, NT, I8>;
-  constexpr int kWarps = F::kWarps, kThreads = kWarps * 32, kQ = 8 * NT;
+  constexpr int kWarps = F::kWarps, kThreads = kWarps * 32, kQ = 8 * NT, kChunkTiles = 4 * kWarps;
   extern __shared__ __align__(1024) uint8_t attn_smem[];      // a name of its own: the swizzle needs this alignment, a shared name takes the first one seen
   uint8_t* const smem = attn_smem;
   __shared__ long long sums[kThreads];          // tiles of the sequences before a thread's own
-  __shared__ long long warp_sums[kWarps];
+  __shared__ long long warp_sums[kWarps], warp_chunks[kWarps], cta_share[4];
   __shared__ int lens[kAttnLens];
   __shared__ AttnPiece pieces[2 * kWarps];
   __shared__ float2 piece_ml[2 * kWarps][kQ];   // {taken off the scores, -infinity without weight; sum of weights}
-  __shared__ int arrived_last;
+  __shared__ float2 run_ml[2 * kWarps][kQ];     // of the run that begins with a piece
+  __shared__ struct { int pieces, first, piece; } joins[2];   // what this CTA joins because it came last
   pdl_launch_dependents();
   pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const int per_seq = a.c.heads * a.blocks, n = a.c.num_seqs;
-  // ---- shares: every CTA adds up the lengths.  chunks: what the items would be in pieces of one tile per warp, the least that a CTA
-  // is worth waking for
+  // ---- shares: every CTA adds up the lengths.  Where the items in chunks of kChunkTiles (four tiles a warp) are no more than the CTAs,
+  // each chunk is a CTA's share: most items are then whole in a CTA, and a join between CTAs costs more than a few tiles.  Otherwise the
+  // CTAs take equal shares of all tiles.
   const int per = (n + kThreads - 1) / kThreads;
   long long mine = 0, mine_chunks = 0;
   for (int i = 0; i < per; ++i) {
@@ -181,32 +196,57 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
     if (raw > a.c.max_pages * a.c.page_size && blockIdx.x == 0) report_index();
     const int tiles = (max(0, min(raw, a.c.max_pages * a.c.page_size)) + kAttnTile - 1) / kAttnTile;
     mine += tiles;
-    mine_chunks += (tiles + kWarps - 1) / kWarps;
+    mine_chunks += (tiles + kChunkTiles - 1) / kChunkTiles;
   }
-  long long upto = mine;
+  long long upto = mine, upto_chunks = mine_chunks;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const long long v = __shfl_up_sync(0xffffffffu, upto, d);
-    if (lane >= d) upto += v;
-    mine_chunks += __shfl_xor_sync(0xffffffffu, mine_chunks, d);
+    const long long v = __shfl_up_sync(0xffffffffu, upto, d), w = __shfl_up_sync(0xffffffffu, upto_chunks, d);
+    if (lane >= d) { upto += v; upto_chunks += w; }
   }
-  __shared__ long long warp_chunks[kWarps];
-  if (lane == 31) { warp_sums[warp] = upto; warp_chunks[warp] = mine_chunks; }
+  if (lane == 31) { warp_sums[warp] = upto; warp_chunks[warp] = upto_chunks; }
   if (tid < 2 * kWarps) pieces[tid].item = -1;
   __syncthreads();
-  long long before = 0, total = 0, chunks_all = 0;
+  long long before = 0, before_chunks = 0, total = 0, chunks_all = 0;
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) before += warp_sums[w];
+    if (w < warp) { before += warp_sums[w]; before_chunks += warp_chunks[w]; }
     total += warp_sums[w];
     chunks_all += warp_chunks[w];
   }
   sums[tid] = before + upto - mine;
-  __syncthreads();
   const long long tiles_all = total * per_seq;
   chunks_all *= per_seq;
-  const int cta = blockIdx.x, used = (int)(chunks_all < gridDim.x ? chunks_all : gridDim.x);
-  const long long c0 = cta < used ? cta * tiles_all / used : 0, c1 = cta < used ? (cta + 1) * tiles_all / used : 0;
+  const int cta = blockIdx.x;
+  AttnShares sh;
+  sh.by_chunk = chunks_all <= gridDim.x;
+  sh.used = sh.by_chunk ? (int)chunks_all : gridDim.x;
+  sh.each = sh.used ? tiles_all / sh.used : 0;
+  sh.more = sh.used ? (int)(tiles_all - sh.each * sh.used) : 0;
+  if (sh.by_chunk) {                                          // chunks are few, and so are sequences: the thread that has this CTA's chunk says so
+    long long first = before_chunks + upto_chunks - mine_chunks, at = sums[tid];
+    if (cta >= first * per_seq && cta < (first + mine_chunks) * per_seq)
+      for (int s = tid * per; s < n && s < (tid + 1) * per; ++s) {
+        const int tiles = (max(0, attn_len(a, lens, s)) + kAttnTile - 1) / kAttnTile, nc = (tiles + kChunkTiles - 1) / kChunkTiles;
+        const int c = cta - (int)(first * per_seq);
+        if (c < nc * per_seq) {
+          const int hb = c / nc, k = c - hb * nc;
+          cta_share[0] = at * per_seq + (long long)hb * tiles + (long long)tiles * k / nc;
+          cta_share[1] = at * per_seq + (long long)hb * tiles + (long long)tiles * (k + 1) / nc;
+          cta_share[2] = cta - k;                             // the CTA of the item's first chunk, ...
+          cta_share[3] = nc;                                  // ... and how many there are
+          break;
+        }
+        first += nc;
+        at += tiles;
+      }
+  }
+  __syncthreads();
+  long long c0 = 0, c1 = 0;
+  if (cta < sh.used) {
+    c0 = sh.by_chunk ? cta_share[0] : sh.begin(cta);
+    c1 = sh.by_chunk ? cta_share[1] : sh.begin(cta + 1);
+  }
   const long long r0 = c0 + (c1 - c0) * warp / kWarps, r1 = c0 + (c1 - c0) * (warp + 1) / kWarps;
   uint8_t* const ring = smem + warp * (F::kStages * F::kStageBytes);
   if (r0 < r1) {
@@ -250,15 +290,25 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
           if (i % F::kChunks >= chunks)
             *reinterpret_cast<uint4*>(ring + s * F::kStageBytes + attn_place<F::kRow>(i / F::kChunks, i % F::kChunks)) = make_uint4(0, 0, 0, 0);
     }
-    auto page_of = [&]() { return __ldcg(a.c.page_table + (long long)pw.seq * a.c.max_pages + pt / tiles_per_page); };
-    int page = page_of();                                     // of tile pt, asked for a tile ahead
+    // page ids of the sequence, a window of 32 at a time: lane i holds the one of page window + i
+    int window = pt / tiles_per_page, ids;
+    auto ask = [&]() {
+      const int at = window + lane, most = (pw.len + a.c.page_size - 1) / a.c.page_size;
+      ids = at < most ? __ldcg(a.c.page_table + (long long)pw.seq * a.c.max_pages + at) : -1;
+    };
+    ask();
     auto issue = [&](int stage) {
       if (more) {
         bool known = true;
         if (run == 0) {                                       // another page
+          const int slot = pt / tiles_per_page, in_page = pt - slot * tiles_per_page;
+          if (slot >= window + 32) {
+            window = slot;
+            ask();
+          }
+          const int page = __shfl_sync(0xffffffffu, ids, slot - window);
           known = (unsigned)page < (unsigned)a.c.num_pages;
           if (!known && lane == 0) report_index();
-          const int in_page = pt % tiles_per_page;
           run = known ? min(tiles_per_page - in_page, pw.t1 - pt) : 1;
           row0 = known ? ((long long)page * a.c.heads + pw.hb / a.blocks) * a.c.page_size + in_page * kAttnTile : 0;
         }
@@ -291,32 +341,25 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
         ++pt;
         if (--run == 0) {
           if (pt == pw.t1) {
+            const int seq = pw.seq;
             more = pw.next(a, lens, per_seq);
             pt = pw.t0;
+            if (more && (pw.seq != seq || window != 0)) {     // from the beginning of another sequence, or of the same one again
+              window = 0;
+              ask();
+            }
           }
-          if (more) page = page_of();
         }
       }
       attn_copy_commit();
     };
-#pragma unroll
-    for (int s = 0; s < F::kStages - 1; ++s) issue(s);
-    int stage = 0, ahead = F::kStages - 1;
-    // ldmatrix addresses: of the keys the matrices (rows 0-7, 8-15) of a piece, then of the next one; of the values (transposed) the same
-    // by pieces first for bf16, whose m-tiles are two pieces, by rows first for int8, whose m-tile is one
-    const int mr = lane & 7, m1 = lane >> 3 & 1, m2 = lane >> 4;
-    const uint32_t k_mat = attn_place<F::kRow>(mr + 8 * m1, m2);
-    const uint32_t v_mat = F::kTileBytes + (I8 ? attn_place<F::kRow>(mr + 8 * m1, m2) : attn_place<F::kRow>(mr + 8 * m2, m1));
-
-    do {
-      // ---- one segment
-      const int head = cw.hb / a.blocks, q0 = (cw.hb - head * a.blocks) * kQ, qn = min(kQ, a.group - q0);
-      uint32_t qf[NT][DP / 16][2];
-      float sc[NT][2];                                        // scores in powers of two per unit of the product, by query column
+    uint32_t qf[NT][DP / 16][2];
+    auto load_q = [&](const AttnWalk& w) {
+      const int head = w.hb / a.blocks, q0 = (w.hb - head * a.blocks) * kQ, qn = min(kQ, a.group - q0);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const int q = nt * 8 + g;
-        const uint16_t* src = a.Q + cw.seq * a.q_stride + (long long)(head * a.group + q0 + q) * a.c.dim;
+        const uint16_t* src = a.Q + w.seq * a.q_stride + (long long)(head * a.group + q0 + q) * a.c.dim;
 #pragma unroll
         for (int k = 0; k < DP / 16; ++k) {
           qf[nt][k][0] = qf[nt][k][1] = 0;
@@ -335,6 +378,27 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
             }
           }
         }
+      }
+    };
+    load_q(cw);                                               // in front of the ring's loads, not behind them
+    bool q_there = true;
+#pragma unroll
+    for (int s = 0; s < F::kStages - 1; ++s) issue(s);
+    int stage = 0, ahead = F::kStages - 1;
+    // ldmatrix addresses: of the keys the matrices (rows 0-7, 8-15) of a piece, then of the next one; of the values (transposed) the same
+    // by pieces first for bf16, whose m-tiles are two pieces, by rows first for int8, whose m-tile is one
+    const int mr = lane & 7, m1 = lane >> 3 & 1, m2 = lane >> 4;
+    const uint32_t k_mat = attn_place<F::kRow>(mr + 8 * m1, m2);
+    const uint32_t v_mat = F::kTileBytes + (I8 ? attn_place<F::kRow>(mr + 8 * m1, m2) : attn_place<F::kRow>(mr + 8 * m2, m1));
+
+    do {
+      // ---- one segment
+      const int head = cw.hb / a.blocks, q0 = (cw.hb - head * a.blocks) * kQ, qn = min(kQ, a.group - q0);
+      if (!q_there) load_q(cw);
+      q_there = false;
+      float sc[NT][2];                                        // scores in powers of two per unit of the product, by query column
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
         sc[nt][0] = sc[nt][1] = a.scale_log2;
         if constexpr (I8) {                                   // to fp16, the largest of the row just below 2^15
           uint32_t top = 0;
@@ -536,93 +600,154 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
   }
   if (c0 >= c1) return;
   __syncthreads();
-  // ---- join in the CTA: runs of pieces of the same item, a unit of four dims of a query head per thread.  Runs are found by every
-  // warp for itself: lane e looks at piece e (there are at most 32).
+  // ---- join in the CTA.  Pieces of one item follow one another: a run.  Every warp finds the runs for itself, lane e looking at piece e.
   const int item_e = lane < 2 * kWarps ? pieces[lane].item : -1;
   const uint32_t have = __ballot_sync(0xffffffffu, item_e >= 0);
   const uint32_t below = have & ((1u << lane) - 1u);
   const int prev = __shfl_sync(0xffffffffu, item_e, below ? 31 - __clz(below) : 0);
-  uint32_t starts = __ballot_sync(0xffffffffu, item_e >= 0 && (below == 0 || prev != item_e));
-  int tail0 = 0, tail1 = 0;                                    // pieces of the items that go on before, behind this CTA (they are joined by the last)
-  AttnPiece run0{}, run1{};
-  constexpr int kUnits = kQ * DP / 4;
-  for (int run = 0; starts; ++run) {
-    const int e0 = __ffs(starts) - 1;
-    starts &= starts - 1;
-    const uint32_t mask = have & ~((1u << e0) - 1u) & (starts ? (1u << (__ffs(starts) - 1)) - 1u : 0xffffffffu);
-    const int e1 = 31 - __clz(mask);
+  const uint32_t starts = __ballot_sync(0xffffffffu, item_e >= 0 && (below == 0 || prev != item_e));
+  const int runs = __popc(starts), qmost = min(kQ, a.group);
+  if (runs == 0) return;
+  auto run_start = [&](int run) {                              // its first piece
+    uint32_t left = starts;
+    for (; run > 0; --run) left &= left - 1;
+    return __ffs(left) - 1;
+  };
+  auto run_mask = [&](int e0) {                                // and all of them
+    const uint32_t later = starts & ~((2u << e0) - 1u);
+    return have & ~((1u << e0) - 1u) & (later ? (1u << (__ffs(later) - 1)) - 1u : 0xffffffffu);
+  };
+  // factors of the pieces: a warp for each run and query head, a lane for each piece
+  for (int k = warp; k < runs * qmost; k += kWarps) {
+    const int q = k % qmost, e0 = run_start(k / qmost);
+    const bool in = run_mask(e0) >> lane & 1;
+    const float2 ml = in ? piece_ml[lane][q] : make_float2(-INFINITY, 0.f);
+    float top = ml.x, l;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    const float f = attn_exp2(ml.x - (top == -INFINITY ? 0.f : top));
+    l = ml.y * f;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+    if (in) piece_ml[lane][q].x = f;
+    if (lane == 0) run_ml[e0][q] = make_float2(top, l);
+  }
+  __syncthreads();
+  // a thread for four dims of a query head of a run
+  const int run_units = qmost * (DP / 4);
+  for (int u = tid; u < runs * run_units; u += kThreads) {
+    const int run = u / run_units, q = (u - run * run_units) / (DP / 4), dim = u % (DP / 4) * 4;
+    const int e0 = run_start(run);
     const AttnPiece pc = pieces[e0];
-    const bool from = pc.whole_from, to = pieces[e1].whole_to;
-    const int head = pc.hb / a.blocks, q0 = (pc.hb - head * a.blocks) * kQ, qn = min(kQ, a.group - q0);
-    for (int u = tid; u < kUnits; u += kThreads) {
-      const int q = u / (DP / 4), dim = u % (DP / 4) * 4;
-      if (q >= qn || dim >= a.c.dim) continue;
-      float top = -INFINITY;
-      for (uint32_t left = mask; left; left &= left - 1) top = fmaxf(top, piece_ml[__ffs(left) - 1][q].x);
-      const float off = top == -INFINITY ? 0.f : top;
-      float4 acc = make_float4(0, 0, 0, 0);
-      float l = 0.f;
-      for (uint32_t left = mask; left; left &= left - 1) {
-        const int e = __ffs(left) - 1;
-        const float2 ml = piece_ml[e][q];
-        const float f = attn_exp2(ml.x - off);
-        l += ml.y * f;
-        const float4 v = e & 1 ? *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(smem + (e >> 1) * (F::kStages * F::kStageBytes)) + q * DP + dim)
-                               : __ldcg(reinterpret_cast<const float4*>(a.warp_part + ((long long)(cta * kWarps + (e >> 1)) * kQ + q) * DP + dim));
-        acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
-      }
-      if (from && to) {
-        const long long qrow = (long long)pc.seq * a.q_heads + head * a.group + q0 + q;
-        attn_store(a, qrow, dim, acc.x, acc.y, acc.z, acc.w, attn_inv(l));
-        if (dim == 0 && a.lse) a.lse[qrow] = attn_lse(top, l);
-      } else {
-        const long long slot = 2 * cta + (from ? 1 : 0);
-        __stcg(reinterpret_cast<float4*>(a.cta_part + (slot * kQ + q) * DP + dim), acc);
-        if (dim == 0) __stcg(a.cta_ml + slot * kQ + q, make_float2(top, l));
-      }
+    const uint32_t mask = run_mask(e0);
+    const int head = pc.hb / a.blocks, q0 = (pc.hb - head * a.blocks) * kQ;
+    if (q0 + q >= a.group || dim >= a.c.dim) continue;
+    float4 acc = make_float4(0, 0, 0, 0);
+    auto add = [&](const float4& v, float f) { acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f; };
+#pragma unroll 4
+    for (int w = e0 >> 1; w < kWarps; ++w) {
+      const uint32_t two = mask >> (2 * w);
+      if (two == 0) break;
+      if (two & 1) add(__ldcg(reinterpret_cast<const float4*>(a.warp_part + ((long long)(cta * kWarps + w) * kQ + q) * DP + dim)), piece_ml[2 * w][q].x);
+      if (two & 2) add(*reinterpret_cast<const float4*>(reinterpret_cast<const float*>(smem + w * (F::kStages * F::kStageBytes)) + q * DP + dim), piece_ml[2 * w + 1][q].x);
     }
-    if (!(from && to)) {                                       // goes on before this CTA, or behind it, or both
-      if (!from) { run0 = pc; tail0 = 1; } else { run1 = pc; tail1 = 1; }
+    const bool from = pc.whole_from, to = pieces[31 - __clz(mask)].whole_to;
+    const float2 ml = run_ml[e0][q];
+    if (from && to) {
+      const long long qrow = (long long)pc.seq * a.q_heads + head * a.group + q0 + q;
+      attn_store(a, qrow, dim, acc.x, acc.y, acc.z, acc.w, attn_inv(ml.y));
+      if (dim == 0 && a.lse) a.lse[qrow] = attn_lse(ml.x, ml.y);
+    } else {
+      const long long slot = 2 * cta + (from ? 1 : 0);
+      __stcg(reinterpret_cast<float4*>(a.cta_part + (slot * kQ + q) * DP + dim), acc);
+      if (dim == 0) __stcg(a.cta_ml + slot * kQ + q, ml);
     }
   }
-  if (!(tail0 | tail1)) return;
-  // ---- join between CTAs: by the last to arrive.  The CTA where the item begins keeps the count.
-  for (int side = 0; side < 2; ++side) {
-    if (!(side ? tail1 : tail0)) continue;
-    const AttnPiece pc = side ? run1 : run0;
-    // the item's tiles, and the CTAs that hold the first and the last of them: CTA c holds x when c tiles_all / used <= x, c the largest such
-    long long base = 0;
-    {
-      const int th = pc.seq / per;
-      base = sums[th];
-      for (int s = th * per; s < pc.seq; ++s) base += (max(0, attn_len(a, lens, s)) + kAttnTile - 1) / kAttnTile;
-    }
-    const int tiles = (attn_len(a, lens, pc.seq) + kAttnTile - 1) / kAttnTile;
-    const long long x0 = base * per_seq + (long long)pc.hb * tiles, x1 = x0 + tiles - 1;
-    const int f0 = (int)(((x0 + 1) * used - 1) / tiles_all), f1 = (int)(((x1 + 1) * used - 1) / tiles_all), np = f1 - f0 + 1;
-    __threadfence();
-    __syncthreads();                                           // this CTA's piece is in memory
-    if (tid == 0) {
-      unsigned long long* const word = a.arrived + f0;
-      unsigned long long seen = *reinterpret_cast<volatile unsigned long long*>(word), put;
+  // ---- join between CTAs: by the last to arrive, for the first run if its item began before this CTA (side 0), for the last one if its
+  // item goes on behind it and began here (side 1).  The CTA where the item begins keeps the count.
+  const int ea = __ffs(starts) - 1, ez = 31 - __clz(starts);
+  const bool open0 = !pieces[ea].whole_from, open1 = pieces[ez].whole_from && !pieces[31 - __clz(have)].whole_to;
+  if (!open0 && !open1) return;
+  __syncthreads();                                             // this CTA's pieces are written
+  if (tid == 0 || tid == 32) {
+    const int side = tid >> 5;
+    joins[side].pieces = 0;
+    if (side ? open1 : open0) {
+      const AttnPiece pc = pieces[side ? ez : ea];
+      int f0, np;
+      if (sh.by_chunk) {
+        f0 = (int)cta_share[2];
+        np = (int)cta_share[3];
+      } else {
+        const int th = pc.seq / per;
+        long long base = sums[th];
+        for (int s = th * per; s < pc.seq; ++s) base += (max(0, attn_len(a, lens, s)) + kAttnTile - 1) / kAttnTile;
+        const int tiles = (attn_len(a, lens, pc.seq) + kAttnTile - 1) / kAttnTile;
+        const long long x0 = base * per_seq + (long long)pc.hb * tiles;
+        f0 = sh.holder(x0);
+        np = sh.holder(x0 + tiles - 1) - f0 + 1;
+      }
+      __threadfence();
+      unsigned long long seen = 0, put;                        // what the last one leaves
       int count;
-      for (;;) {                                               // ends: every failure is another CTA's success, and there are np of those
+      for (;;) {                                               // ends: every failure is another CTA's success, of which there are np
         count = (seen >> 16) == (a.call >> 16) ? (int)(seen & 0xffff) + 1 : 1;
         put = count == np ? 0 : a.call | (unsigned)count;
-        const unsigned long long got = atomicCAS(word, seen, put);
+        const unsigned long long got = atomicCAS(a.arrived + f0, seen, put);
         if (got == seen) break;
         seen = got;
       }
       __threadfence();
-      arrived_last = count == np;
+      if (count == np) joins[side] = {np, f0, side ? ez : ea};
     }
-    __syncthreads();
-    if (!arrived_last) continue;
+  }
+  __syncthreads();
+  for (int side = 0; side < 2; ++side) {
+    const int np = joins[side].pieces, f0 = joins[side].first;
+    if (np == 0) continue;
+    const AttnPiece pc = pieces[joins[side].piece];
     const int head = pc.hb / a.blocks, q0 = (pc.hb - head * a.blocks) * kQ, qn = min(kQ, a.group - q0);
-    // weights of the pieces into shared memory (the rings are free), then the units, split over the pieces where threads are left
+    auto slot_of = [&](int i) { return (long long)(2 * (f0 + i) + (i == 0 ? 1 : 0)); };
+    auto out = [&](int q, int dim, const float4& acc, float top, float l) {
+      const long long qrow = (long long)pc.seq * a.q_heads + head * a.group + q0 + q;
+      attn_store(a, qrow, dim, acc.x, acc.y, acc.z, acc.w, attn_inv(l));
+      if (dim == 0 && a.lse) a.lse[qrow] = attn_lse(top, l);
+    };
+    const int units = qn * (DP / 4);
+    if (np <= kFewPieces) {                                    // one trip to memory
+      for (int u = tid; u < units; u += kThreads) {
+        const int q = u / (DP / 4), dim = u % (DP / 4) * 4;
+        if (dim >= a.c.dim) continue;
+        float2 ml[kFewPieces];
+        float4 v[kFewPieces];
+#pragma unroll
+        for (int i = 0; i < kFewPieces; ++i) {
+          ml[i] = make_float2(-INFINITY, 0.f);
+          v[i] = make_float4(0, 0, 0, 0);
+          if (i < np) {
+            ml[i] = __ldcg(&a.cta_ml[slot_of(i) * kQ + q]);
+            v[i] = __ldcg(reinterpret_cast<const float4*>(a.cta_part + (slot_of(i) * kQ + q) * DP + dim));
+          }
+        }
+        float top = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int i = 0; i < kFewPieces; ++i) top = fmaxf(top, ml[i].x);
+        const float off = top == -INFINITY ? 0.f : top;
+        float4 acc = make_float4(0, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < kFewPieces; ++i) {
+          const float f = attn_exp2(ml[i].x - off);
+          l += ml[i].y * f;
+          acc.x += v[i].x * f; acc.y += v[i].y * f; acc.z += v[i].z * f; acc.w += v[i].w * f;
+        }
+        out(q, dim, acc, top, l);
+      }
+      continue;
+    }
+    // factors into shared memory (the rings are free), then the units, split over the pieces where threads are left
+    __syncthreads();
     float* const fac = reinterpret_cast<float*>(smem);         // [np][kQ]
     float* const tops = fac + np * kQ;                         // [kQ] top, [kQ] l
-    auto slot_of = [&](int i) { return (long long)(2 * (f0 + i) + (i == 0 ? 1 : 0)); };
     for (int q = warp; q < qn; q += kWarps) {
       float top = -INFINITY, l = 0.f;
       for (int i = lane; i < np; i += 32) top = fmaxf(top, __ldcg(&a.cta_ml[slot_of(i) * kQ + q]).x);
@@ -640,7 +765,6 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
       if (lane == 0) { tops[q] = top; tops[kQ + q] = l; }
     }
     __syncthreads();
-    const int units = qn * (DP / 4);
     int split = 1;                                             // threads that share a unit's pieces: a power of two, in one warp
     while (split < 32 && units * split * 2 <= kThreads && split < np) split *= 2;
     for (int u0 = 0; u0 < units; u0 += kThreads / split) {
@@ -658,11 +782,7 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
         acc.x += __shfl_xor_sync(0xffffffffu, acc.x, d); acc.y += __shfl_xor_sync(0xffffffffu, acc.y, d);
         acc.z += __shfl_xor_sync(0xffffffffu, acc.z, d); acc.w += __shfl_xor_sync(0xffffffffu, acc.w, d);
       }
-      if (u < units && dim < a.c.dim && part == 0) {
-        const long long qrow = (long long)pc.seq * a.q_heads + head * a.group + q0 + q;
-        attn_store(a, qrow, dim, acc.x, acc.y, acc.z, acc.w, attn_inv(tops[kQ + q]));
-        if (dim == 0 && a.lse) a.lse[qrow] = attn_lse(tops[q], tops[kQ + q]);
-      }
+      if (u < units && dim < a.c.dim && part == 0) out(q, dim, acc, tops[q], tops[kQ + q]);
     }
     __syncthreads();
   }
