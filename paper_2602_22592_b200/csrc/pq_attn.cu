@@ -24,6 +24,7 @@
 //     maximum of that, so that they stay in range, and the sum of weights puts gamma_v back.
 #include <cuda_fp16.h>
 
+#include <algorithm>
 #include <atomic>
 #include <chrono>
 #include <mutex>
@@ -33,7 +34,8 @@
 namespace pq {
 
 constexpr int kAttnTile = 16;                 // positions of a tile; pages are multiples of it
-constexpr int kAttnRingBytes = 208 * 1024;
+constexpr int kAttnRingBytes = 204 * 1024;    // of 227 KB a CTA can have, 18 of them static
+constexpr int kAttnSmemMost = 209 * 1024;
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
 template <int DP, int NT, bool I8>
@@ -69,6 +71,21 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// A word that counts arrivals of one launch: the launch's number above 16 bits, the count below.  Whoever is going to count first makes
+// sure that the word is this launch's (a failed exchange means that another CTA of it did), so that the workspace may hold anything before.
+__device__ __forceinline__ void count_open(unsigned long long* word, unsigned long long call) {
+  const unsigned long long seen = *reinterpret_cast<volatile unsigned long long*>(word);
+  if (seen >> 16 != call >> 16) atomicCAS(word, seen, call);
+}
+// One more: releases what the CTA has written (behind its barrier) and acquires what those before it have.  The last one leaves 0.
+__device__ __forceinline__ bool count_last(unsigned long long* word, int of) {
+  unsigned long long old;
+  asm volatile("atom.acq_rel.gpu.global.add.u64 %0, [%1], 1;" : "=l"(old) : "l"(word) : "memory");
+  const bool last = (int)(old & 0xffff) == of - 1;
+  if (last) *reinterpret_cast<volatile unsigned long long*>(word) = 0;
+  return last;
+}
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p) : "memory"); }
 __device__ __forceinline__ float attn_exp2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float attn_log2(float x) { float y; asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float attn_rcp(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
@@ -98,6 +115,18 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
 }
 constexpr float kWeightTop = 14.f;        // int8 caches: the largest weight is 2^14, so that small ones keep their bits in fp16
 
+// Division by a number that the host knows, of 0 <= n < 2^31: multiply and shift (Granlund and Montgomery's round-up method)
+struct FastDiv {
+  uint32_t d, mul, shift;
+  FastDiv() = default;
+  explicit FastDiv(uint32_t by) : d(by), shift(0) {
+    while ((1ull << shift) < by) ++shift;
+    mul = (uint32_t)(((1ull << 32) * ((1ull << shift) - by)) / by + 1);
+  }
+  __device__ int operator()(int n) const { return (int)((__umulhi((uint32_t)n, mul) + (uint32_t)n) >> shift); }
+  __device__ long long wide(long long n) const { return n >> 31 ? n / d : (long long)operator()((int)n); }
+};
+
 struct AttnArgs {
   KvCache c;
   const uint16_t* Q;
@@ -108,6 +137,8 @@ struct AttnArgs {
   float scale_log2;          // scale x log2(e): weights are powers of two
   int q_heads, group;        // query heads, and of them per cache head
   int blocks;                // column blocks of 8 NT query heads per cache head
+  FastDiv by_blocks, by_per_seq, by_page_tiles, by_chunks;   // blocks, heads x blocks, tiles of a page, 16-byte pieces of a row
+  int first_in_smem;         // a warp's first piece fits in shared memory, behind the rings
   // workspace
   float* warp_part;          // [CTAs x warps][8 NT][DP] unnormalised sums of a warp's first piece, if that is not its last
   float* cta_part;           // [2 CTAs][8 NT][DP] the same of a CTA: 2 c + 1 where its piece is the item's beginning, 2 c elsewhere
@@ -178,11 +209,33 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
   __shared__ AttnPiece pieces[2 * kWarps];
   __shared__ float2 piece_ml[2 * kWarps][kQ];   // {taken off the scores, -infinity without weight; sum of weights}
   __shared__ float2 run_ml[2 * kWarps][kQ];     // of the run that begins with a piece
-  __shared__ struct { int pieces, first, piece; } joins[2];   // what this CTA joins because it came last
+  __shared__ struct { int first, pieces, piece; } open[2];    // items shared with CTAs before, behind: the CTA where it begins, how many hold it; what to join
   pdl_launch_dependents();
-  pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-  const int per_seq = a.c.heads * a.blocks, n = a.c.num_seqs;
+  const int per_seq = a.by_per_seq.d, n = a.c.num_seqs, row_bytes = a.c.pitch * (I8 ? 1 : 2), chunks = row_bytes / 16;
+  uint8_t* const ring = smem + warp * (F::kStages * F::kStageBytes);
+      // copy i takes this lane's piece 32 i + lane of the tile, whose rows are neighbours in the page
+      uint32_t place[F::kCopies];
+  #pragma unroll
+      for (int i = 0; i < F::kCopies; ++i) {
+        const int at = 32 * i + lane, r = a.by_chunks(at);
+        place[i] = attn_place<F::kRow>(r, at - r * chunks);
+      }
+      if (chunks < F::kChunks) {                                // pieces behind the rows' end are never copied: zeros once and for all
+        for (int s = 0; s < F::kStages; ++s)
+          for (int i = lane; i < kAttnTile * F::kChunks; i += 32)
+            if (i % F::kChunks >= chunks)
+              *reinterpret_cast<uint4*>(ring + s * F::kStageBytes + attn_place<F::kRow>(i / F::kChunks, i % F::kChunks)) = make_uint4(0, 0, 0, 0);
+      }
+  // lengths, page ids and queries are trips to memory one after another: ask for them to be in L2 (where later writes reach them too)
+  {
+    const long long line = (long long)(blockIdx.x * kThreads + tid) * 128;
+    if (line < (long long)n * 4) prefetch_l2(reinterpret_cast<const uint8_t*>(a.lens) + line);
+    if (line < (long long)n * a.c.max_pages * 4) prefetch_l2(reinterpret_cast<const uint8_t*>(a.c.page_table) + line);
+    if (line < ((long long)(n - 1) * a.q_stride + (long long)a.q_heads * a.c.dim) * 2) prefetch_l2(reinterpret_cast<const uint8_t*>(a.Q) + line);
+  }
+  pdl_wait();
+  auto first_at = [&](int w) { return reinterpret_cast<float*>(smem + F::kSmem) + w * min(kQ, a.group) * DP; };
   // ---- shares: every CTA adds up the lengths.  Where the items in chunks of kChunkTiles (four tiles a warp) are no more than the CTAs,
   // each chunk is a CTA's share: most items are then whole in a CTA, and a join between CTAs costs more than a few tiles.  Otherwise the
   // CTAs take equal shares of all tiles.
@@ -221,7 +274,7 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
   AttnShares sh;
   sh.by_chunk = chunks_all <= gridDim.x;
   sh.used = sh.by_chunk ? (int)chunks_all : gridDim.x;
-  sh.each = sh.used ? tiles_all / sh.used : 0;
+  sh.each = sh.used == 0 ? 0 : tiles_all >> 31 ? tiles_all / sh.used : (long long)((uint32_t)tiles_all / (uint32_t)sh.used);
   sh.more = sh.used ? (int)(tiles_all - sh.each * sh.used) : 0;
   if (sh.by_chunk) {                                          // chunks are few, and so are sequences: the thread that has this CTA's chunk says so
     long long first = before_chunks + upto_chunks - mine_chunks, at = sums[tid];
@@ -247,11 +300,10 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
     c0 = sh.by_chunk ? cta_share[0] : sh.begin(cta);
     c1 = sh.by_chunk ? cta_share[1] : sh.begin(cta + 1);
   }
-  const long long r0 = c0 + (c1 - c0) * warp / kWarps, r1 = c0 + (c1 - c0) * (warp + 1) / kWarps;
-  uint8_t* const ring = smem + warp * (F::kStages * F::kStageBytes);
+  const long long r0 = c0 + (unsigned long long)((c1 - c0) * warp) / kWarps, r1 = c0 + (unsigned long long)((c1 - c0) * (warp + 1)) / kWarps;
   if (r0 < r1) {
     // ---- first segment: the sequence whose tiles hold r0
-    const long long x = r0 / per_seq;                         // compared per sequence, not per head
+    const long long x = a.by_per_seq.wide(r0);                         // compared per sequence, not per head
     int lo = 0, hi = kThreads;                                // last thread whose sequences begin at or before it
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
@@ -267,7 +319,7 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
       base += cw.tiles;
     }
     const long long in_seq = r0 - base * per_seq;
-    cw.hb = (int)(in_seq / cw.tiles);
+    cw.hb = in_seq >> 31 ? (int)(in_seq / cw.tiles) : (int)((uint32_t)in_seq / (uint32_t)cw.tiles);
     cw.t0 = (int)(in_seq - (long long)cw.hb * cw.tiles);
     cw.t1 = (int)(cw.tiles - cw.t0 < r1 - r0 ? cw.tiles : cw.t0 + (r1 - r0));
     cw.left = r1 - r0 - (cw.t1 - cw.t0);
@@ -275,23 +327,10 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
     int pt = cw.t0, run = 0;                                  // next tile to load, and how many more of its page
     bool more = true;
     long long row0 = 0;                                       // its first row
-    const int tiles_per_page = a.c.page_size / kAttnTile, row_bytes = a.c.pitch * (I8 ? 1 : 2), chunks = row_bytes / 16;
+    const int tiles_per_page = a.by_page_tiles.d;
     const uint32_t ring_at = smem_u32(ring), gamma_at = smem_u32(smem) + F::kGammaAt + warp * (F::kStages * F::kGammaBytes);
-    // copy i takes this lane's piece 32 i + lane of the tile, whose rows are neighbours in the page
-    uint32_t place[F::kCopies];
-#pragma unroll
-    for (int i = 0; i < F::kCopies; ++i) {
-      const int at = 32 * i + lane, r = at / chunks;
-      place[i] = attn_place<F::kRow>(r, at - r * chunks);
-    }
-    if (chunks < F::kChunks) {                                // pieces behind the rows' end are never copied: zeros once and for all
-      for (int s = 0; s < F::kStages; ++s)
-        for (int i = lane; i < kAttnTile * F::kChunks; i += 32)
-          if (i % F::kChunks >= chunks)
-            *reinterpret_cast<uint4*>(ring + s * F::kStageBytes + attn_place<F::kRow>(i / F::kChunks, i % F::kChunks)) = make_uint4(0, 0, 0, 0);
-    }
     // page ids of the sequence, a window of 32 at a time: lane i holds the one of page window + i
-    int window = pt / tiles_per_page, ids;
+    int window = a.by_page_tiles(pt), ids;
     auto ask = [&]() {
       const int at = window + lane, most = (pw.len + a.c.page_size - 1) / a.c.page_size;
       ids = at < most ? __ldcg(a.c.page_table + (long long)pw.seq * a.c.max_pages + at) : -1;
@@ -301,7 +340,7 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
       if (more) {
         bool known = true;
         if (run == 0) {                                       // another page
-          const int slot = pt / tiles_per_page, in_page = pt - slot * tiles_per_page;
+          const int slot = a.by_page_tiles(pt), in_page = pt - slot * tiles_per_page;
           if (slot >= window + 32) {
             window = slot;
             ask();
@@ -310,7 +349,7 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
           known = (unsigned)page < (unsigned)a.c.num_pages;
           if (!known && lane == 0) report_index();
           run = known ? min(tiles_per_page - in_page, pw.t1 - pt) : 1;
-          row0 = known ? ((long long)page * a.c.heads + pw.hb / a.blocks) * a.c.page_size + in_page * kAttnTile : 0;
+          row0 = known ? ((long long)page * a.c.heads + a.by_blocks(pw.hb)) * a.c.page_size + in_page * kAttnTile : 0;
         }
         const int rows = known ? pw.len - pt * kAttnTile : 0;
         const uint8_t* const kp = static_cast<const uint8_t*>(a.c.K) + row0 * row_bytes + lane * 16;
@@ -355,7 +394,7 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
     };
     uint32_t qf[NT][DP / 16][2];
     auto load_q = [&](const AttnWalk& w) {
-      const int head = w.hb / a.blocks, q0 = (w.hb - head * a.blocks) * kQ, qn = min(kQ, a.group - q0);
+      const int head = a.by_blocks(w.hb), q0 = (w.hb - head * a.blocks) * kQ, qn = min(kQ, a.group - q0);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const int q = nt * 8 + g;
@@ -384,6 +423,16 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
     bool q_there = true;
 #pragma unroll
     for (int s = 0; s < F::kStages - 1; ++s) issue(s);
+    // counts of the items that this CTA may share: the one that it begins inside of, and one that begins here (while the first loads are on their way)
+    if (lane == 0 && (r0 == c0 || r1 == c1)) {
+      if (r0 == c0 && cw.t0 > 0) {
+        const long long x0 = r0 - cw.t0;
+        open[0].first = sh.by_chunk ? (int)cta_share[2] : sh.holder(x0);
+        open[0].pieces = sh.by_chunk ? (int)cta_share[3] : sh.holder(x0 + cw.tiles - 1) - open[0].first + 1;
+        count_open(a.arrived + open[0].first, a.call);
+      }
+      if (r1 == c1) count_open(a.arrived + cta, a.call);
+    }
     int stage = 0, ahead = F::kStages - 1;
     // ldmatrix addresses: of the keys the matrices (rows 0-7, 8-15) of a piece, then of the next one; of the values (transposed) the same
     // by pieces first for bf16, whose m-tiles are two pieces, by rows first for int8, whose m-tile is one
@@ -393,7 +442,7 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
 
     do {
       // ---- one segment
-      const int head = cw.hb / a.blocks, q0 = (cw.hb - head * a.blocks) * kQ, qn = min(kQ, a.group - q0);
+      const int head = a.by_blocks(cw.hb), q0 = (cw.hb - head * a.blocks) * kQ, qn = min(kQ, a.group - q0);
       if (!q_there) load_q(cw);
       q_there = false;
       float sc[NT][2];                                        // scores in powers of two per unit of the product, by query column
@@ -553,11 +602,17 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], d);
       const bool whole = cw.t0 == 0 && cw.t1 == cw.tiles, last = cw.left == 0;
-      float* const part = last ? reinterpret_cast<float*>(ring) : a.warp_part + (long long)(cta * kWarps + warp) * kQ * DP;
+      float* const part = last ? reinterpret_cast<float*>(ring) : a.first_in_smem ? first_at(warp) : a.warp_part + (long long)(cta * kWarps + warp) * kQ * DP;
       const int at = 2 * warp + (last ? 1 : 0);
       if (!whole) {
         if (last) { attn_copy_wait<0>(); __syncwarp(); }
-        if (lane == 0) pieces[at] = AttnPiece{cw.seq * per_seq + cw.hb, cw.seq, cw.hb, cw.t0 == 0, cw.t1 == cw.tiles};
+        if (lane == 0) {
+          pieces[at] = AttnPiece{cw.seq * per_seq + cw.hb, cw.seq, cw.hb, cw.t0 == 0, cw.t1 == cw.tiles};
+          if (last && r1 == c1 && cw.t1 < cw.tiles) {          // the CTA's share ends inside: if the item began here, how many CTAs hold it
+            open[1].first = cta;
+            open[1].pieces = sh.by_chunk ? (int)cta_share[3] : sh.holder(c1 + (cw.tiles - cw.t1) - 1) - cta + 1;
+          }
+        }
       }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -640,16 +695,22 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
     const int e0 = run_start(run);
     const AttnPiece pc = pieces[e0];
     const uint32_t mask = run_mask(e0);
-    const int head = pc.hb / a.blocks, q0 = (pc.hb - head * a.blocks) * kQ;
+    const int head = a.by_blocks(pc.hb), q0 = (pc.hb - head * a.blocks) * kQ;
     if (q0 + q >= a.group || dim >= a.c.dim) continue;
     float4 acc = make_float4(0, 0, 0, 0);
     auto add = [&](const float4& v, float f) { acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f; };
+    auto last_of = [&](int w) { return *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(smem + w * (F::kStages * F::kStageBytes)) + q * DP + dim); };
+    for (uint32_t left = mask & 0x55555555u; left; left &= left - 1) {
+      const int e = __ffs(left) - 1;
+      add(a.first_in_smem ? *reinterpret_cast<const float4*>(first_at(e >> 1) + q * DP + dim)
+                          : __ldcg(reinterpret_cast<const float4*>(a.warp_part + ((long long)(cta * kWarps + (e >> 1)) * kQ + q) * DP + dim)), piece_ml[e][q].x);
+    }
+    const uint32_t lasts = mask & 0xaaaaaaaau;
+    if (lasts) {
+      const int w0 = (__ffs(lasts) - 1) >> 1, w1 = (31 - __clz(lasts)) >> 1;
 #pragma unroll 4
-    for (int w = e0 >> 1; w < kWarps; ++w) {
-      const uint32_t two = mask >> (2 * w);
-      if (two == 0) break;
-      if (two & 1) add(__ldcg(reinterpret_cast<const float4*>(a.warp_part + ((long long)(cta * kWarps + w) * kQ + q) * DP + dim)), piece_ml[2 * w][q].x);
-      if (two & 2) add(*reinterpret_cast<const float4*>(reinterpret_cast<const float*>(smem + w * (F::kStages * F::kStageBytes)) + q * DP + dim), piece_ml[2 * w + 1][q].x);
+      for (int w = w0; w <= w1; ++w)
+        if (lasts >> (2 * w + 1) & 1) add(last_of(w), piece_ml[2 * w + 1][q].x);
     }
     const bool from = pc.whole_from, to = pieces[31 - __clz(mask)].whole_to;
     const float2 ml = run_ml[e0][q];
@@ -671,42 +732,15 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
   __syncthreads();                                             // this CTA's pieces are written
   if (tid == 0 || tid == 32) {
     const int side = tid >> 5;
-    joins[side].pieces = 0;
-    if (side ? open1 : open0) {
-      const AttnPiece pc = pieces[side ? ez : ea];
-      int f0, np;
-      if (sh.by_chunk) {
-        f0 = (int)cta_share[2];
-        np = (int)cta_share[3];
-      } else {
-        const int th = pc.seq / per;
-        long long base = sums[th];
-        for (int s = th * per; s < pc.seq; ++s) base += (max(0, attn_len(a, lens, s)) + kAttnTile - 1) / kAttnTile;
-        const int tiles = (attn_len(a, lens, pc.seq) + kAttnTile - 1) / kAttnTile;
-        const long long x0 = base * per_seq + (long long)pc.hb * tiles;
-        f0 = sh.holder(x0);
-        np = sh.holder(x0 + tiles - 1) - f0 + 1;
-      }
-      __threadfence();
-      unsigned long long seen = 0, put;                        // what the last one leaves
-      int count;
-      for (;;) {                                               // ends: every failure is another CTA's success, of which there are np
-        count = (seen >> 16) == (a.call >> 16) ? (int)(seen & 0xffff) + 1 : 1;
-        put = count == np ? 0 : a.call | (unsigned)count;
-        const unsigned long long got = atomicCAS(a.arrived + f0, seen, put);
-        if (got == seen) break;
-        seen = got;
-      }
-      __threadfence();
-      if (count == np) joins[side] = {np, f0, side ? ez : ea};
-    }
+    open[side].piece = -1;
+    if ((side ? open1 : open0) && count_last(a.arrived + open[side].first, open[side].pieces)) open[side].piece = side ? ez : ea;
   }
   __syncthreads();
   for (int side = 0; side < 2; ++side) {
-    const int np = joins[side].pieces, f0 = joins[side].first;
-    if (np == 0) continue;
-    const AttnPiece pc = pieces[joins[side].piece];
-    const int head = pc.hb / a.blocks, q0 = (pc.hb - head * a.blocks) * kQ, qn = min(kQ, a.group - q0);
+    if (open[side].piece < 0) continue;
+    const int np = open[side].pieces, f0 = open[side].first;
+    const AttnPiece pc = pieces[open[side].piece];
+    const int head = a.by_blocks(pc.hb), q0 = (pc.hb - head * a.blocks) * kQ, qn = min(kQ, a.group - q0);
     auto slot_of = [&](int i) { return (long long)(2 * (f0 + i) + (i == 0 ? 1 : 0)); };
     auto out = [&](int q, int dim, const float4& acc, float top, float l) {
       const long long qrow = (long long)pc.seq * a.q_heads + head * a.group + q0 + q;
@@ -792,11 +826,11 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
 // host side
 // ---------------------------------------------------------------------------
 using AttnKernel = void (*)(AttnArgs);
-struct AttnChoice { AttnKernel kernel; int smem, warps; };
+struct AttnChoice { AttnKernel kernel; int smem, warps, most; };     // rings; and what a CTA can ask for at most beside its static share
 template <int DP, int NT>
 static AttnChoice attn_choice(bool i8) {
-  return i8 ? AttnChoice{k_attn_decode<DP, NT, true>, AttnForm<DP, NT, true>::kSmem, AttnForm<DP, NT, true>::kWarps}
-            : AttnChoice{k_attn_decode<DP, NT, false>, AttnForm<DP, NT, false>::kSmem, AttnForm<DP, NT, false>::kWarps};
+  return i8 ? AttnChoice{k_attn_decode<DP, NT, true>, AttnForm<DP, NT, true>::kSmem, AttnForm<DP, NT, true>::kWarps, kAttnSmemMost}
+            : AttnChoice{k_attn_decode<DP, NT, false>, AttnForm<DP, NT, false>::kSmem, AttnForm<DP, NT, false>::kWarps, kAttnSmemMost};
 }
 static AttnChoice attn_choice(int dp, int nt, bool i8) {
   if (dp == 64) return nt == 1 ? attn_choice<64, 1>(i8) : attn_choice<64, 2>(i8);
@@ -853,7 +887,7 @@ static cudaError_t attn_limits() {
         for (int i8 = 0; i8 < 2; ++i8) {
           if (result[dev] != cudaSuccess) return;
           const AttnChoice ch = attn_choice(dp, nt, i8);
-          result[dev] = cudaFuncSetAttribute(ch.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ch.smem);
+          result[dev] = cudaFuncSetAttribute(ch.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ch.most);
         }
   });
   return result[dev];
@@ -867,10 +901,16 @@ cudaError_t launch_attn_decode(const KvCache& c, int q_heads, const uint16_t* Q,
   a.c = c; a.Q = Q; a.q_stride = q_stride; a.lens = lens; a.O = O; a.lse = lse;
   a.scale_log2 = scale * kLog2e;
   a.q_heads = q_heads; a.group = q_heads / c.heads; a.blocks = p.blocks;
+  a.by_blocks = FastDiv(p.blocks);
+  a.by_per_seq = FastDiv(c.heads * p.blocks);
+  a.by_page_tiles = FastDiv(c.page_size / kAttnTile);
+  a.by_chunks = FastDiv(c.pitch * (c.format == PQ_KV_INT8 ? 1 : 2) / 16);
+  const size_t firsts = (size_t)p.choice.warps * std::min(a.group, 8 * p.nt) * p.dp * 4;
+  a.first_in_smem = p.choice.smem + firsts <= (size_t)p.choice.most;
   a.call = attn_call_number();
   attn_carve(p, ws, &a);
   LaunchScope ls(KID_ATTN_DECODE, st);
-  return launch_pdl(p.choice.kernel, sm_count(), p.choice.warps * 32, p.choice.smem, st, a);
+  return launch_pdl(p.choice.kernel, sm_count(), p.choice.warps * 32, p.choice.smem + (a.first_in_smem ? firsts : 0), st, a);
 }
 
 }  // namespace pq
