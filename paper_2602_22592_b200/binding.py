@@ -412,34 +412,40 @@ def pq_linear_backward(d, dY, X, w_s8, w_scales, A, B, Wr, alpha, beta, saved, d
         _ptr(ws), _nbytes(ws), _stream(stream)))
 
 
-def _rows(fn, name, t, rows, width):
-    """Row stride in values of a 2-D (or packed, contiguous) bf16 tensor of `rows` rows of `width` values."""
-    if t.dtype != torch.bfloat16:
-        raise PqArgumentError(fn, f"{name} has to be bfloat16")
-    if t.dim() == 2 and t.shape[0] == rows and t.shape[1] == width and t.stride(1) == 1:
-        return t.stride(0) if rows > 1 else 0      # the stride of a single row means nothing
-    if t.is_contiguous() and t.numel() == rows * width:
-        return 0
-    raise PqArgumentError(fn, f"{name} has to hold {rows} rows of {width} values, each of them contiguous")
-
-
-def _need(fn, name, t, dtype, numel):
-    if t.dtype != dtype or t.numel() != numel or not t.is_contiguous():
+def _at(fn, name, t, dtype, numel, dev):
+    """Address of a contiguous tensor of `numel` `dtype` values on the current device `dev`, where the kernel will run; None stays None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != numel or not t.is_contiguous():
         raise PqArgumentError(fn, f"{name} has to be a contiguous tensor of {numel} {dtype} values")
+    if t.get_device() != dev:
+        raise PqArgumentError(fn, f"{name} is on {t.device}, the current device is cuda:{dev}")
+    return t.data_ptr()
 
 
-def _same_device(fn, *tensors):
-    """A kernel is launched on the current device: every tensor has to live there."""
-    dev = _device()
-    for t in tensors:
-        if t is not None and (t.device.type != "cuda" or t.device.index != dev):
-            raise PqArgumentError(fn, f"a tensor is on {t.device}, the current device is cuda:{dev}")
+def _rows_at(fn, name, t, rows, width, dev):
+    """Address and row stride in values (0: dense) of `rows` rows of `width` bf16 values, each of them contiguous."""
+    if t.is_contiguous():
+        return _at(fn, name, t, torch.bfloat16, rows * width, dev), 0
+    if t.dtype is not torch.bfloat16 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width or t.stride(1) != 1:
+        raise PqArgumentError(fn, f"{name} has to hold {rows} rows of {width} bfloat16 values, each of them contiguous")
+    if t.get_device() != dev:
+        raise PqArgumentError(fn, f"{name} is on {t.device}, the current device is cuda:{dev}")
+    return t.data_ptr(), t.stride(0) if rows > 1 else 0      # the stride of a single row means nothing
+
+
+def _whole(fn, name, t, parts):
+    """How many times `parts` values a tensor holds."""
+    n = t.numel()
+    if parts < 1 or n % parts:
+        raise PqArgumentError(fn, f"{name} has to hold a multiple of {parts} values")
+    return n // parts
 
 
 def make_kv_cache(K, V, page_table, head_dim, k_gamma=None, v_gamma=None) -> pq_kv_cache:
     """The cache whose pages are K, V [pages, heads, page_size, pitch] (bf16, or int8 with k_gamma, v_gamma [pages, heads,
     page_size] fp32) and whose sequences' pages stand in page_table [sequences, entries] int32.  pitch = pq_kv_pitch(format, head_dim).
-    The struct only holds pointers: it keeps the tensors alive, and they must not be resized while it is in use."""
+    The struct holds pointers and, as `tensors`, the tensors they point into."""
     fn = "make_kv_cache"
     int8 = K.dtype == torch.int8
     if K.dim() != 4 or K.dtype not in (torch.bfloat16, torch.int8) or not K.is_contiguous():
@@ -447,20 +453,15 @@ def make_kv_cache(K, V, page_table, head_dim, k_gamma=None, v_gamma=None) -> pq_
     pages, heads, page_size, pitch = K.shape
     if pitch != pq_kv_pitch(PQ_KV_INT8 if int8 else PQ_KV_BF16, head_dim):
         raise PqArgumentError(fn, f"rows of {pitch} values do not fit heads of {head_dim}")
-    _need(fn, "V", V, K.dtype, K.numel())
     if int8 != (k_gamma is not None) or int8 != (v_gamma is not None):
         raise PqArgumentError(fn, "an int8 cache has k_gamma and v_gamma, a bfloat16 cache neither")
-    if int8:
-        _need(fn, "k_gamma", k_gamma, torch.float32, pages * heads * page_size)
-        _need(fn, "v_gamma", v_gamma, torch.float32, pages * heads * page_size)
     if page_table.dim() != 2:
         raise PqArgumentError(fn, "page_table has to be [sequences, entries]")
-    _need(fn, "page_table", page_table, torch.int32, page_table.numel())
-    if len({t.device for t in (K, V, page_table, k_gamma, v_gamma) if t is not None}) > 1:
-        raise PqArgumentError(fn, "the cache's tensors are on several devices")
-    c = pq_kv_cache(ctypes.sizeof(pq_kv_cache), 0, PQ_KV_INT8 if int8 else PQ_KV_BF16, heads, head_dim, page_size, pages, page_table.shape[0],
-                    page_table.shape[1], 0, K.data_ptr(), V.data_ptr(), k_gamma.data_ptr() if int8 else None, v_gamma.data_ptr() if int8 else None,
-                    page_table.data_ptr())
+    dev = K.get_device()
+    at = [_at(fn, "K", K, K.dtype, K.numel(), dev), _at(fn, "V", V, K.dtype, K.numel(), dev)]
+    at += [_at(fn, n, g, torch.float32, pages * heads * page_size, dev) for n, g in (("k_gamma", k_gamma), ("v_gamma", v_gamma))]
+    at.append(_at(fn, "page_table", page_table, torch.int32, page_table.numel(), dev))
+    c = pq_kv_cache(ctypes.sizeof(pq_kv_cache), 0, PQ_KV_INT8 if int8 else PQ_KV_BF16, heads, head_dim, page_size, pages, *page_table.shape, 0, *at)
     c.tensors = (K, V, page_table, k_gamma, v_gamma)
     return c
 
@@ -469,40 +470,47 @@ def pq_kv_pitch(format: int, head_dim: int) -> int:
     return lib().pq_kv_pitch(format, head_dim)
 
 
+def _cache_device(fn, cache):
+    dev = _device()
+    if cache.tensors[0].get_device() != dev:
+        raise PqArgumentError(fn, f"the cache is on {cache.tensors[0].device}, the current device is cuda:{dev}")
+    return dev
+
+
 def pq_kv_append(cache, seq, pos, K, V, cos=None, sin=None, Q=None, Q_out=None, stream=None):
     """Write tokens to the cache (rotated by cos, sin [rows, head_dim / 2] fp32 where given), and rotate their queries Q into Q_out.
     K, V, Q: [tokens, heads * head_dim] bf16, rows of any stride; seq, pos: [tokens] int32."""
-    fn, n, width = "pq_kv_append", seq.numel(), cache.heads * cache.head_dim
-    _same_device(fn, cache.tensors[0], seq, pos, K, V, cos, sin, Q, Q_out)
-    _need(fn, "seq", seq, torch.int32, n)
-    _need(fn, "pos", pos, torch.int32, n)
+    fn, n, dim = "pq_kv_append", seq.numel(), cache.head_dim
+    dev = _cache_device(fn, cache)
+    s, p = _at(fn, "seq", seq, torch.int32, n, dev), _at(fn, "pos", pos, torch.int32, n, dev)
+    k, k_stride = _rows_at(fn, "K", K, n, cache.heads * dim, dev)
+    v, v_stride = _rows_at(fn, "V", V, n, cache.heads * dim, dev)
     rope_rows = q_heads = q_stride = 0
-    if cos is not None and sin is not None:
-        rope_rows = cos.numel() // (cache.head_dim // 2)
-        _need(fn, "cos", cos, torch.float32, rope_rows * (cache.head_dim // 2))
-        _need(fn, "sin", sin, torch.float32, cos.numel())
-    if Q is not None and Q_out is not None and n > 0:
-        q_heads = Q_out.numel() // (n * cache.head_dim)
-        _need(fn, "Q_out", Q_out, torch.bfloat16, n * q_heads * cache.head_dim)
-        q_stride = _rows(fn, "Q", Q, n, q_heads * cache.head_dim)
-    if n == 0:
-        return
-    _check(fn, lib().pq_kv_append(ctypes.byref(cache), n, _ptr(seq), _ptr(pos), _ptr(K), _rows(fn, "K", K, n, width), _ptr(V),
-                                  _rows(fn, "V", V, n, width), _ptr(cos), _ptr(sin), rope_rows, _ptr(Q), q_stride, q_heads, _ptr(Q_out),
-                                  _stream(stream)))
+    c = d = q = q_out = None
+    if cos is not None or sin is not None:
+        if cos is None or sin is None:
+            raise PqArgumentError(fn, "cos and sin come together")
+        rope_rows = _whole(fn, "cos", cos, dim // 2)
+        c, d = _at(fn, "cos", cos, torch.float32, rope_rows * (dim // 2), dev), _at(fn, "sin", sin, torch.float32, rope_rows * (dim // 2), dev)
+    if Q is not None or Q_out is not None:
+        if Q is None or Q_out is None:
+            raise PqArgumentError(fn, "Q and Q_out come together")
+        if n:
+            q_heads = _whole(fn, "Q_out", Q_out, n * dim)
+            q, q_stride = _rows_at(fn, "Q", Q, n, q_heads * dim, dev)
+            q_out = _at(fn, "Q_out", Q_out, torch.bfloat16, n * q_heads * dim, dev)
+    if n:      # an empty tensor has no address
+        _check(fn, lib().pq_kv_append(ctypes.byref(cache), n, s, p, k, k_stride, v, v_stride, c, d, rope_rows, q, q_stride, q_heads, q_out, _stream(stream)))
 
 
 def pq_kv_read(cache, seq, pos, K_out, V_out, stream=None):
     """K_out, V_out [tokens, heads * head_dim] bf16: what the cache holds at (seq, pos)."""
-    fn, n = "pq_kv_read", seq.numel()
-    _same_device(fn, cache.tensors[0], seq, pos, K_out, V_out)
-    _need(fn, "seq", seq, torch.int32, n)
-    _need(fn, "pos", pos, torch.int32, n)
-    _need(fn, "K_out", K_out, torch.bfloat16, n * cache.heads * cache.head_dim)
-    _need(fn, "V_out", V_out, torch.bfloat16, n * cache.heads * cache.head_dim)
-    if n == 0:
-        return
-    _check(fn, lib().pq_kv_read(ctypes.byref(cache), n, _ptr(seq), _ptr(pos), _ptr(K_out), _ptr(V_out), _stream(stream)))
+    fn, n, width = "pq_kv_read", seq.numel(), cache.heads * cache.head_dim
+    dev = _cache_device(fn, cache)
+    s, p = _at(fn, "seq", seq, torch.int32, n, dev), _at(fn, "pos", pos, torch.int32, n, dev)
+    k, v = _at(fn, "K_out", K_out, torch.bfloat16, n * width, dev), _at(fn, "V_out", V_out, torch.bfloat16, n * width, dev)
+    if n:
+        _check(fn, lib().pq_kv_read(ctypes.byref(cache), n, s, p, k, v, _stream(stream)))
 
 
 def pq_attn_workspace_bytes(cache, q_heads: int) -> int:
@@ -512,35 +520,27 @@ def pq_attn_workspace_bytes(cache, q_heads: int) -> int:
 def pq_attn_decode(cache, Q, lens, scale, O, lse, ws, stream=None):
     """One token per sequence of the cache's page table: O [sequences, q_heads * head_dim] bf16 (and lse [sequences, q_heads] fp32, or None)
     from Q of that shape (rows of any stride) over the first lens[s] positions."""
-    fn, n = "pq_attn_decode", cache.num_seqs
-    _same_device(fn, cache.tensors[0], Q, lens, O, lse, ws)
-    q_heads = O.numel() // (n * cache.head_dim)
-    _need(fn, "O", O, torch.bfloat16, n * q_heads * cache.head_dim)
-    _need(fn, "lens", lens, torch.int32, n)
-    if lse is not None:
-        _need(fn, "lse", lse, torch.float32, n * q_heads)
-    _check(fn, lib().pq_attn_decode(ctypes.byref(cache), q_heads, _ptr(Q), _rows(fn, "Q", Q, n, q_heads * cache.head_dim), _ptr(lens), scale, _ptr(O),
-                                    _ptr(lse), _ptr(ws), _nbytes(ws), _stream(stream)))
+    fn, n, dim = "pq_attn_decode", cache.num_seqs, cache.head_dim
+    dev = _cache_device(fn, cache)
+    q_heads = _whole(fn, "O", O, n * dim)
+    q, q_stride = _rows_at(fn, "Q", Q, n, q_heads * dim, dev)
+    _check(fn, lib().pq_attn_decode(ctypes.byref(cache), q_heads, q, q_stride, _at(fn, "lens", lens, torch.int32, n, dev), scale,
+                                    _at(fn, "O", O, torch.bfloat16, n * q_heads * dim, dev), _at(fn, "lse", lse, torch.float32, n * q_heads, dev),
+                                    _at(fn, "ws", ws, torch.uint8, ws.numel(), dev), ws.numel(), _stream(stream)))
 
 
 def make_norm_desc(T, N, eps=1e-5, res_scale=1.0, gate_vector=False) -> pq_norm_desc:
     return pq_norm_desc(ctypes.sizeof(pq_norm_desc), PQ_SCALE_VECTOR if gate_vector else 0, T, N, eps, res_scale)
 
 
-def _norm_arguments(fn, d, rows, weights, sums, gates):
-    _same_device(fn, *rows.values(), *weights.values(), *sums.values(), *gates.values())
-    for kind, dtype, numel in ((rows, torch.bfloat16, d.T * d.N), (weights, torch.bfloat16, d.N), (sums, torch.float32, d.N),
-                               (gates, torch.float32, d.N if d.flags & PQ_SCALE_VECTOR else 1)):
-        for name, t in kind.items():
-            if t is not None:
-                _need(fn, name, t, dtype, numel)
-
-
 def pq_block_norm_forward(d, x, y, post_weight, gate, pre_weight, x_out, h, stream=None):
     """x_out = res_scale x + gate (rms(y) post_weight), h = rms(x_out) pre_weight; what is None is left out (see pquant.h)."""
-    _norm_arguments("pq_block_norm_forward", d, dict(x=x, y=y, x_out=x_out, h=h), dict(post_weight=post_weight, pre_weight=pre_weight), {}, dict(gate=gate))
-    _check("pq_block_norm_forward", lib().pq_block_norm_forward(ctypes.byref(d), _ptr(x), _ptr(y), _ptr(post_weight), _ptr(gate), _ptr(pre_weight),
-                                                                 _ptr(x_out), _ptr(h), _stream(stream)))
+    fn, N, dev, bf = "pq_block_norm_forward", d.N, _device(), torch.bfloat16
+    all_ = d.T * N
+    _check(fn, lib().pq_block_norm_forward(
+        ctypes.byref(d), _at(fn, "x", x, bf, all_, dev), _at(fn, "y", y, bf, all_, dev), _at(fn, "post_weight", post_weight, bf, N, dev),
+        _at(fn, "gate", gate, torch.float32, N if d.flags & PQ_SCALE_VECTOR else 1, dev), _at(fn, "pre_weight", pre_weight, bf, N, dev),
+        _at(fn, "x_out", x_out, bf, all_, dev), _at(fn, "h", h, bf, all_, dev), _stream(stream)))
 
 
 def pq_block_norm_workspace_bytes(d: pq_norm_desc) -> int:
@@ -549,12 +549,14 @@ def pq_block_norm_workspace_bytes(d: pq_norm_desc) -> int:
 
 def pq_block_norm_backward(d, dx_out, dh, x_out, y, post_weight, gate, pre_weight, dx, dy, dpost, dgate, dpre, ws, stream=None):
     """Gradients of pq_block_norm_forward; every one that is given is overwritten."""
-    _norm_arguments("pq_block_norm_backward", d, dict(dx_out=dx_out, dh=dh, x_out=x_out, y=y, dx=dx, dy=dy), dict(post_weight=post_weight, pre_weight=pre_weight),
-                    dict(dpost=dpost, dpre=dpre), dict(gate=gate, dgate=dgate))
-    _same_device("pq_block_norm_backward", ws)
-    _check("pq_block_norm_backward", lib().pq_block_norm_backward(
-        ctypes.byref(d), _ptr(dx_out), _ptr(dh), _ptr(x_out), _ptr(y), _ptr(post_weight), _ptr(gate), _ptr(pre_weight), _ptr(dx), _ptr(dy), _ptr(dpost),
-        _ptr(dgate), _ptr(dpre), _ptr(ws), _nbytes(ws), _stream(stream)))
+    fn, N, dev, bf, f32 = "pq_block_norm_backward", d.N, _device(), torch.bfloat16, torch.float32
+    all_, gates = d.T * N, N if d.flags & PQ_SCALE_VECTOR else 1
+    _check(fn, lib().pq_block_norm_backward(
+        ctypes.byref(d), _at(fn, "dx_out", dx_out, bf, all_, dev), _at(fn, "dh", dh, bf, all_, dev), _at(fn, "x_out", x_out, bf, all_, dev),
+        _at(fn, "y", y, bf, all_, dev), _at(fn, "post_weight", post_weight, bf, N, dev), _at(fn, "gate", gate, f32, gates, dev),
+        _at(fn, "pre_weight", pre_weight, bf, N, dev), _at(fn, "dx", dx, bf, all_, dev), _at(fn, "dy", dy, bf, all_, dev),
+        _at(fn, "dpost", dpost, f32, N, dev), _at(fn, "dgate", dgate, f32, gates, dev), _at(fn, "dpre", dpre, f32, N, dev),
+        _at(fn, "ws", ws, torch.uint8, ws.numel(), dev), ws.numel(), _stream(stream)))
 
 
 def pq_debug_gemm(mode, M, N, K, A, B, D, stream=None):

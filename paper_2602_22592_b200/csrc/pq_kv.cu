@@ -44,7 +44,7 @@ __device__ __forceinline__ void store_bf16(uint16_t* p, const float (&v)[VEC]) {
     *reinterpret_cast<uint32_t*>(p) = pack_bf16x2(v[0], v[1]);
 }
 
-constexpr int kSteps = 4;        // of a unit
+constexpr int kSteps = 4;        // of a unit at most; with few rows one, so that they spread over more warps
 
 // The raw bits of VEC bf16 values
 template <int VEC> struct Raw;
@@ -60,10 +60,13 @@ __device__ __forceinline__ void raw_floats(const Raw<8>& r, float (&v)[8]) {
 }
 __device__ __forceinline__ void raw_floats(const Raw<2>& r, float (&v)[2]) { v[0] = bf16lo(r.v); v[1] = bf16hi(r.v); }
 
-// A warp's walk over units = (token, rows of it).  Indices of the unit behind the current one are asked for early.
+// A warp's walk over units = (token, rows of it).  While a unit is worked on, the place of the next one is looked up and the position and
+// sequence of the one behind it are on their way.
 struct KvWalk {
-  long long unit, stride, units;
-  int per_token, tok, part, at, sq;      // of the next unit
+  long long unit, stride, units;      // the unit whose position has been asked for
+  int per_token, tok1, part1, at1, sq1;
+  int tok, part, at;                  // the current unit, ...
+  int2 place;                         // ... and its place: page < 0 if there is none, or nothing to do (at < 0)
   __device__ void begin(int tokens, int per_token_, const int* seq, const int* pos) {
     per_token = per_token_;
     units = (long long)tokens * per_token;
@@ -73,10 +76,17 @@ struct KvWalk {
   }
   __device__ void ask(const int* seq, const int* pos) {
     if (unit >= units) return;
-    tok = units >> 31 ? (int)(unit / per_token) : (int)((uint32_t)unit / (uint32_t)per_token);
-    part = (int)(unit - (long long)tok * per_token);
-    at = __ldcg(pos + tok);
-    sq = __ldcg(seq + tok);
+    tok1 = units >> 31 ? (int)(unit / per_token) : (int)((uint32_t)unit / (uint32_t)per_token);
+    part1 = (int)(unit - (long long)tok1 * per_token);
+    at1 = __ldcg(pos + tok1);
+    sq1 = __ldcg(seq + tok1);
+  }
+  __device__ bool more() const { return unit < units; }
+  __device__ void next(const KvCache& c, const int* seq, const int* pos) {
+    tok = tok1; part = part1; at = at1;
+    place = at1 >= 0 ? kv_place(c, sq1, at1) : make_int2(-1, 0);
+    unit += stride;
+    ask(seq, pos);
   }
 };
 
@@ -89,10 +99,10 @@ struct KvWalk {
 // gamma = NaN and reads back as NaN throughout.
 // VEC = 8 (16-byte accesses) where both halves are multiples of 8 values and the rows are 16-byte aligned, else 2.
 // ---------------------------------------------------------------------------
-template <int VEC, int G>
+template <int VEC, int G, bool I8>
 __global__ void __launch_bounds__(256, VEC == 8 ? 2 : 3) k_kv_append(KvCache c, int tokens, const int* seq, const int* pos, const uint16_t* K, long long k_stride,
                                                       const uint16_t* V, long long v_stride, const float* cos_t, const float* sin_t, int rope_rows,
-                                                      const uint16_t* Q, long long q_stride, int q_heads, uint16_t* Q_out) {
+                                                      const uint16_t* Q, long long q_stride, int q_heads, uint16_t* Q_out, int steps) {
   pdl_launch_dependents();
   pdl_wait();
   constexpr int kMost = VEC == 8 ? 1 : 2;                              // pieces of VEC pairs per lane (G = 16: head_dim <= 128)
@@ -100,40 +110,35 @@ __global__ void __launch_bounds__(256, VEC == 8 ? 2 : 3) k_kv_append(KvCache c, 
   const int lane = threadIdx.x % G, sub = threadIdx.x % 32 / G, half = c.dim / 2, pieces = half / VEC;
   const int rows = q_heads + 2 * c.heads;
   const unsigned mask = G == 32 ? 0xffffffffu : ((1u << (G & 31)) - 1u) << (sub * G);
+  const long long head_rows = (long long)c.page_size * c.pitch;       // values from head to head of a page
   KvWalk w;
-  w.begin(tokens, (rows + kRows * kSteps - 1) / (kRows * kSteps), seq, pos);
-  while (w.unit < w.units) {
-    const int tok = w.tok, at = w.at, sq = w.sq, row0 = w.part * (kRows * kSteps) + sub;
-    // the rows do not wait for the indices
+  w.begin(tokens, (rows + kRows * steps - 1) / (kRows * steps), seq, pos);
+  if (!w.more()) return;
+  w.next(c, seq, pos);
+  for (bool more = true; more;) {
+    const int tok = w.tok, at = w.at, row0 = w.part * (kRows * steps) + sub;
+    const int2 place = w.place;
+    const uint16_t* const q_row = Q + tok * q_stride;
+    const uint16_t* const k_row = K + tok * k_stride - (long long)q_heads * c.dim;                  // of row r: + r dim
+    const uint16_t* const v_row = V + tok * v_stride - (long long)(q_heads + c.heads) * c.dim;
     Raw<VEC> ra[kSteps][kMost], rb[kSteps][kMost];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
       const int r = row0 + s * kRows;
-      const uint16_t* src = r < q_heads ? Q + tok * q_stride + (long long)r * c.dim
-                            : r < q_heads + c.heads ? K + tok * k_stride + (long long)(r - q_heads) * c.dim
-                                                    : V + tok * v_stride + (long long)(r - q_heads - c.heads) * c.dim;
+      const uint16_t* src = (r < q_heads ? q_row : r < q_heads + c.heads ? k_row : v_row) + (long long)r * c.dim + lane * VEC;
 #pragma unroll
-      for (int i = 0; i < kMost; ++i) {
-        const int p = lane + i * G;
-        if (r < rows && p < pieces) { load_raw<VEC>(src + p * VEC, ra[s][i]); load_raw<VEC>(src + half + p * VEC, rb[s][i]); }
-      }
+      for (int i = 0; i < kMost; ++i)
+        if (s < steps && r < rows && lane + i * G < pieces) { load_raw<VEC>(src + i * G * VEC, ra[s][i]); load_raw<VEC>(src + half + i * G * VEC, rb[s][i]); }
     }
-    w.unit += w.stride;
-    w.ask(seq, pos);
-    if (at < 0) continue;                           // padding: nothing of this token is written
-    const int2 place = kv_place(c, sq, at);
-    if (place.x < 0 || (cos_t && at >= rope_rows)) {
-      if (threadIdx.x % 32 == 0) report_index();
-      continue;
-    }
+    // other warps turn other rows of the token by the same angles: through L1
     float cs[kMost][VEC], sn[kMost][VEC];
+    const bool turns = cos_t && at >= 0 && at < rope_rows;
 #pragma unroll
     for (int i = 0; i < kMost; ++i) {
       const int p = lane + i * G;
-      if (!cos_t || p >= pieces) continue;
+      if (!turns || p >= pieces) continue;
       const float* cr = cos_t + (long long)at * half + p * VEC;
       const float* sr = sin_t + (long long)at * half + p * VEC;
-      // other warps turn other rows of the token by the same angles: through L1
       if constexpr (VEC == 8) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -146,11 +151,18 @@ __global__ void __launch_bounds__(256, VEC == 8 ? 2 : 3) k_kv_append(KvCache c, 
         cs[i][0] = x.x; cs[i][1] = x.y; sn[i][0] = y.x; sn[i][1] = y.y;
       }
     }
+    more = w.more();
+    if (more) w.next(c, seq, pos);
+    if (place.x < 0 || (cos_t && at >= rope_rows)) {                   // nothing of this token is written: padding, or no such place
+      if (at >= 0 && threadIdx.x % 32 == 0) report_index();
+      continue;
+    }
+    const long long crow0 = kv_row(c, place, 0);
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
       const int r = row0 + s * kRows;
-      if (r >= rows) break;
-      const int kind = r < q_heads ? 0 : r < q_heads + c.heads ? 1 : 2;      // query, key, value
+      if (s >= steps || r >= rows) break;
+      const bool query = r < q_heads, key = r < q_heads + c.heads;     // else a value
       float a[kMost][VEC], b[kMost][VEC];
       uint32_t amax = 0;
 #pragma unroll
@@ -158,43 +170,42 @@ __global__ void __launch_bounds__(256, VEC == 8 ? 2 : 3) k_kv_append(KvCache c, 
         if (lane + i * G >= pieces) continue;
         raw_floats(ra[s][i], a[i]);
         raw_floats(rb[s][i], b[i]);
-        if (cos_t && kind < 2) {
-#pragma unroll
-          for (int k = 0; k < VEC; ++k) {
-            const float u = __fsub_rn(__fmul_rn(a[i][k], cs[i][k]), __fmul_rn(b[i][k], sn[i][k]));
-            const float v = __fadd_rn(__fmul_rn(b[i][k], cs[i][k]), __fmul_rn(a[i][k], sn[i][k]));
-            a[i][k] = u;
-            b[i][k] = v;
-          }
+        if (turns && key) {
 #pragma unroll
           for (int k = 0; k < VEC; k += 2) {
-            const uint32_t x = pack_bf16x2(a[i][k], a[i][k + 1]), y = pack_bf16x2(b[i][k], b[i][k + 1]);
+            float u[2], v[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              u[j] = __fsub_rn(__fmul_rn(a[i][k + j], cs[i][k + j]), __fmul_rn(b[i][k + j], sn[i][k + j]));
+              v[j] = __fadd_rn(__fmul_rn(b[i][k + j], cs[i][k + j]), __fmul_rn(a[i][k + j], sn[i][k + j]));
+            }
+            const uint32_t x = pack_bf16x2(u[0], u[1]), y = pack_bf16x2(v[0], v[1]);
             a[i][k] = bf16lo(x); a[i][k + 1] = bf16hi(x);
             b[i][k] = bf16lo(y); b[i][k + 1] = bf16hi(y);
           }
         }
+        if (I8) {
 #pragma unroll
-        for (int k = 0; k < VEC; ++k)      // as integers: a NaN is above infinity is above the rest
-          amax = max(amax, max(__float_as_uint(a[i][k]) & 0x7fffffffu, __float_as_uint(b[i][k]) & 0x7fffffffu));
+          for (int k = 0; k < VEC; ++k)      // as integers: a NaN is above infinity is above the rest
+            amax = max(amax, max(__float_as_uint(a[i][k]) & 0x7fffffffu, __float_as_uint(b[i][k]) & 0x7fffffffu));
+        }
       }
-      const int head = kind == 0 ? r : kind == 1 ? r - q_heads : r - q_heads - c.heads;
-      const long long crow = kv_row(c, place, head);
-      if (kind == 0 || c.format == PQ_KV_BF16) {
-        uint16_t* dst = kind == 0 ? Q_out + ((long long)tok * q_heads + head) * c.dim : static_cast<uint16_t*>(kind == 1 ? c.K : c.V) + crow * c.pitch;
+      const int head = query ? r : key ? r - q_heads : r - q_heads - c.heads;
+      if (query || !I8) {
+        uint16_t* dst = query ? Q_out + ((long long)tok * q_heads + head) * c.dim : static_cast<uint16_t*>(key ? c.K : c.V) + crow0 * c.pitch + head * head_rows;
 #pragma unroll
         for (int i = 0; i < kMost; ++i) {
           const int p = lane + i * G;
           if (p < pieces) { store_bf16<VEC>(dst + p * VEC, a[i]); store_bf16<VEC>(dst + half + p * VEC, b[i]); }
         }
-        if (kind != 0)
-          for (int i = c.dim + lane; i < c.pitch; i += G) dst[i] = 0;
+        if (!query && lane < c.pitch - c.dim) dst[c.dim + lane] = 0;      // at most 4 of them
         continue;
       }
 #pragma unroll
       for (int d = G / 2; d > 0; d >>= 1) amax = max(amax, __shfl_xor_sync(mask, amax, d));
       const bool finite = amax < 0x7f800000u;
       const float gamma = finite ? __fdiv_rn(kActQmax, fmaxf(__uint_as_float(amax), kActAmaxFloor)) : __uint_as_float(0x7fffffffu);
-      int8_t* dst = static_cast<int8_t*>(kind == 1 ? c.K : c.V) + crow * c.pitch;
+      int8_t* dst = static_cast<int8_t*>(key ? c.K : c.V) + crow0 * c.pitch + head * head_rows;
       auto code = [&](float x) { return finite ? sat_s8(__fmul_rn(x, gamma)) & 0xff : 0; };
 #pragma unroll
       for (int i = 0; i < kMost; ++i) {
@@ -214,7 +225,7 @@ __global__ void __launch_bounds__(256, VEC == 8 ? 2 : 3) k_kv_append(KvCache c, 
         put(dst + half + p * VEC, b[i]);
       }
       for (int i = c.dim + lane; i < c.pitch; i += G) dst[i] = 0;
-      if (lane == 0) (kind == 1 ? c.k_gamma : c.v_gamma)[crow] = gamma;
+      if (lane == 0) (key ? c.k_gamma : c.v_gamma)[crow0 + (long long)head * c.page_size] = gamma;
     }
   }
 }
@@ -225,82 +236,69 @@ __global__ void __launch_bounds__(256, VEC == 8 ? 2 : 3) k_kv_append(KvCache c, 
 // give the rounded quotient): three instructions a value where a division takes about ten, which would be
 // more than the memory asks for.
 // ---------------------------------------------------------------------------
-template <int VEC, int G>
-__global__ void __launch_bounds__(256, 4) k_kv_read(KvCache c, int tokens, const int* seq, const int* pos, uint16_t* K_out, uint16_t* V_out) {
+template <int VEC, int G, bool I8>
+__global__ void __launch_bounds__(256, I8 ? 5 : 4) k_kv_read(KvCache c, int tokens, const int* seq, const int* pos, uint16_t* K_out, uint16_t* V_out, int steps) {
   pdl_launch_dependents();
   pdl_wait();
   constexpr int kMost = VEC == 8 ? 1 : 2;                              // pieces per lane (G = 16: head_dim <= 128)
-  constexpr int kRows = 32 / G;
+  constexpr int kRows = 32 / G, kBytes = I8 ? 1 : 2;
+  using In = Raw<I8 ? VEC / 2 : VEC>;                                  // the bytes of VEC values
   const int lane = threadIdx.x % G, sub = threadIdx.x % 32 / G, pieces = c.dim / VEC, rows = 2 * c.heads;
+  const long long head_bytes = (long long)c.page_size * c.pitch * kBytes;
   KvWalk w;
-  w.begin(tokens, (rows + kRows * kSteps - 1) / (kRows * kSteps), seq, pos);
-  auto locate = [&](int& tok, int& row0, int& at) -> int2 {            // of the unit that the walk stands at; moves on
-    tok = w.tok; at = w.at; row0 = w.part * (kRows * kSteps) + sub;
-    const int2 p = at >= 0 ? kv_place(c, w.sq, at) : make_int2(-1, 0);
-    w.unit += w.stride;
-    w.ask(seq, pos);
-    return p;
-  };
-  if (w.unit >= w.units) return;
-  int tok, row0, at;
-  int2 place = locate(tok, row0, at);
+  w.begin(tokens, (rows + kRows * steps - 1) / (kRows * steps), seq, pos);
+  if (!w.more()) return;
+  w.next(c, seq, pos);
   for (bool more = true; more;) {
-    int tok1 = 0, row1 = 0, at1 = -1;
-    int2 place1 = make_int2(-1, 0);
-    const bool bf = c.format == PQ_KV_BF16;
-    Raw<VEC> raw[kSteps][kMost];                                       // bf16 rows; of int8 rows the first half of the bits
+    const int tok = w.tok, row0 = w.part * (kRows * steps) + sub;
+    const int2 place = w.place;
+    if (place.x < 0 && w.at >= 0 && threadIdx.x % 32 == 0) report_index();
+    In raw[kSteps][kMost];
     float gamma[kSteps];
     if (place.x >= 0) {
+      const long long crow0 = kv_row(c, place, 0);
+      const uint8_t* const k_src = static_cast<const uint8_t*>(c.K) + crow0 * c.pitch * kBytes + lane * VEC * kBytes;
+      const uint8_t* const v_src = static_cast<const uint8_t*>(c.V) + crow0 * c.pitch * kBytes + lane * VEC * kBytes;
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
-        const int r = row0 + s * kRows;
-        if (r >= rows) break;
-        const bool key = r < c.heads;
-        const long long crow = kv_row(c, place, key ? r : r - c.heads);
-        const uint8_t* src = static_cast<const uint8_t*>(key ? c.K : c.V) + crow * c.pitch * (bf ? 2 : 1);
+        const int r = row0 + s * kRows, head = r < c.heads ? r : r - c.heads;
+        if (s >= steps || r >= rows) break;
+        const uint8_t* src = (r < c.heads ? k_src : v_src) + head * head_bytes;
 #pragma unroll
-        for (int i = 0; i < kMost; ++i) {
-          const int p = lane + i * G;
-          if (p >= pieces) continue;
-          if (bf) load_raw<VEC>(reinterpret_cast<const uint16_t*>(src) + p * VEC, raw[s][i]);
-          else if constexpr (VEC == 8) { const uint2 u = __ldcg(reinterpret_cast<const uint2*>(src) + p); raw[s][i].v = make_uint4(u.x, u.y, 0, 0); }
-          else raw[s][i].v.x = __ldcg(reinterpret_cast<const uint32_t*>(src) + p);
-        }
-        if (!bf) gamma[s] = __ldcg((key ? c.k_gamma : c.v_gamma) + crow);
+        for (int i = 0; i < kMost; ++i)
+          if (lane + i * G < pieces) raw[s][i].v = __ldcg(reinterpret_cast<const decltype(raw[s][i].v)*>(src + i * G * VEC * kBytes));
+        if (I8) gamma[s] = __ldcg((r < c.heads ? c.k_gamma : c.v_gamma) + crow0 + (long long)head * c.page_size);
       }
-    } else if (at >= 0 && threadIdx.x % 32 == 0) {
-      report_index();
     }
-    more = w.unit < w.units;
-    if (more) place1 = locate(tok1, row1, at1);                        // its page id is on the way while this unit's rows are
-    if (place.x >= 0) {
+    more = w.more();
+    if (more) w.next(c, seq, pos);
+    if (place.x < 0) continue;
+    const long long out0 = (long long)tok * c.heads * c.dim + lane * VEC;
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        const int r = row0 + s * kRows;
-        if (r >= rows) break;
-        const bool key = r < c.heads;
-        uint16_t* dst = (key ? K_out : V_out) + ((long long)tok * c.heads + (key ? r : r - c.heads)) * c.dim;
-        const float inv = bf ? 0.f : __frcp_rn(gamma[s]);
+    for (int s = 0; s < kSteps; ++s) {
+      const int r = row0 + s * kRows, head = r < c.heads ? r : r - c.heads;
+      if (s >= steps || r >= rows) break;
+      uint16_t* const dst = (r < c.heads ? K_out : V_out) + out0 + head * c.dim;
+      const float inv = I8 ? __frcp_rn(gamma[s]) : 0.f;
 #pragma unroll
-        for (int i = 0; i < kMost; ++i) {
-          const int p = lane + i * G;
-          if (p >= pieces) continue;
-          if (bf) {
-            *reinterpret_cast<decltype(raw[s][i].v)*>(dst + p * VEC) = raw[s][i].v;
-          } else {
-            float v[VEC];
-            const uint32_t word[2] = {raw[s][i].v.x, raw[s][i].v.y};
+      for (int i = 0; i < kMost; ++i) {
+        if (lane + i * G >= pieces) continue;
+        if constexpr (!I8) {
+          *reinterpret_cast<decltype(raw[s][i].v)*>(dst + i * G * VEC) = raw[s][i].v;
+        } else {
+          uint32_t word[VEC / 4];
+          if constexpr (VEC == 8) { word[0] = raw[s][i].v.x; word[1] = raw[s][i].v.y; } else word[0] = raw[s][i].v;
+          float v[VEC];
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-              const float x = (float)(int8_t)(word[k / 4] >> (8 * (k % 4)) & 0xff), q = __fmul_rn(x, inv);
-              v[k] = __fmaf_rn(__fmaf_rn(-q, gamma[s], x), inv, q);
-            }
-            store_bf16<VEC>(dst + p * VEC, v);
+          for (int k = 0; k < VEC; ++k) {
+            // under the bits of 2^23 an integer below it is itself: conversions by permute and addition
+            const float x = __uint_as_float(__byte_perm(word[k / 4] ^ 0x80808080u, 0x4B000000u, 0x7440 + k % 4)) - 8388736.f, q = __fmul_rn(x, inv);
+            v[k] = __fmaf_rn(__fmaf_rn(-q, gamma[s], x), inv, q);
           }
+          store_bf16<VEC>(dst + i * G * VEC, v);
         }
       }
     }
-    place = place1; tok = tok1; row0 = row1; at = at1;
   }
 }
 
@@ -310,10 +308,25 @@ static int group_of(int pieces) {
   while (g < pieces && g < 32) g *= 2;
   return g;
 }
-// Units of kSteps x (32 / g) rows, eight warps a block, as many blocks as can be resident
-static int blocks_for(int tokens, int rows, int g, int resident) {
-  const int per_token = (rows + 32 / g * kSteps - 1) / (32 / g * kSteps);
+// Rows of a warp's unit in steps of 32 / g: one step while the warps of a block per SM have one unit or less each
+static int steps_for(int tokens, int rows, int g) {
+  return (long long)tokens * ((rows + 32 / g - 1) / (32 / g)) <= 8LL * sm_count() ? 1 : kSteps;
+}
+// eight warps a block, as many blocks as can be resident
+static int blocks_for(int tokens, int rows, int g, int steps, int resident) {
+  const int per_token = (rows + 32 / g * steps - 1) / (32 / g * steps);
   return (int)std::min<long long>(((long long)tokens * per_token + 7) / 8, (long long)sm_count() * resident);
+}
+
+template <bool I8>
+static auto append_kernel(bool wide, int g) {
+  return !wide ? (g == 16 ? k_kv_append<2, 16, I8> : k_kv_append<2, 32, I8>)
+         : g == 2 ? k_kv_append<8, 2, I8> : g == 4 ? k_kv_append<8, 4, I8> : g == 8 ? k_kv_append<8, 8, I8> : k_kv_append<8, 16, I8>;
+}
+template <bool I8>
+static auto read_kernel(bool wide, int g) {
+  return !wide ? (g == 16 ? k_kv_read<4, 16, I8> : k_kv_read<4, 32, I8>)
+         : g == 2 ? k_kv_read<8, 2, I8> : g == 4 ? k_kv_read<8, 4, I8> : g == 8 ? k_kv_read<8, 8, I8> : g == 16 ? k_kv_read<8, 16, I8> : k_kv_read<8, 32, I8>;
 }
 
 cudaError_t launch_kv_append(const KvCache& c, int tokens, const int* seq, const int* pos, const uint16_t* K, long long k_stride,
@@ -321,19 +334,20 @@ cudaError_t launch_kv_append(const KvCache& c, int tokens, const int* seq, const
                              long long q_stride, int q_heads, uint16_t* Q_out, cudaStream_t st) {
   const bool wide = c.dim % 16 == 0 && k_stride % 8 == 0 && v_stride % 8 == 0 && (!Q || q_stride % 8 == 0);
   const int g = wide ? group_of(c.dim / 16) : c.dim <= 128 ? 16 : 32;
-  auto kern = !wide ? (g == 16 ? k_kv_append<2, 16> : k_kv_append<2, 32>) : g == 2 ? k_kv_append<8, 2> : g == 4 ? k_kv_append<8, 4> : g == 8 ? k_kv_append<8, 8> : k_kv_append<8, 16>;
+  auto kern = c.format == PQ_KV_INT8 ? append_kernel<true>(wide, g) : append_kernel<false>(wide, g);
+  const int steps = steps_for(tokens, q_heads + 2 * c.heads, g);
   LaunchScope ls(KID_KV_APPEND, st);
-  return launch_pdl(kern, blocks_for(tokens, q_heads + 2 * c.heads, g, wide ? 2 : 3), 256, 0, st, c, tokens, seq, pos, K, k_stride, V, v_stride,
-                    cos_t, sin_t, rope_rows, Q, q_stride, q_heads, Q_out);
+  return launch_pdl(kern, blocks_for(tokens, q_heads + 2 * c.heads, g, steps, wide ? 2 : 3), 256, 0, st, c, tokens, seq, pos, K, k_stride, V, v_stride,
+                    cos_t, sin_t, rope_rows, Q, q_stride, q_heads, Q_out, steps);
 }
 
 cudaError_t launch_kv_read(const KvCache& c, int tokens, const int* seq, const int* pos, uint16_t* K_out, uint16_t* V_out, cudaStream_t st) {
   const bool wide = c.dim % 8 == 0;
   const int g = wide ? group_of(c.dim / 8) : c.dim <= 128 ? 16 : 32;
-  auto kern = !wide ? (g == 16 ? k_kv_read<4, 16> : k_kv_read<4, 32>)
-              : g == 2 ? k_kv_read<8, 2> : g == 4 ? k_kv_read<8, 4> : g == 8 ? k_kv_read<8, 8> : g == 16 ? k_kv_read<8, 16> : k_kv_read<8, 32>;
+  auto kern = c.format == PQ_KV_INT8 ? read_kernel<true>(wide, g) : read_kernel<false>(wide, g);
+  const int steps = steps_for(tokens, 2 * c.heads, g);
   LaunchScope ls(KID_KV_READ, st);
-  return launch_pdl(kern, blocks_for(tokens, 2 * c.heads, g, 4), 256, 0, st, c, tokens, seq, pos, K_out, V_out);
+  return launch_pdl(kern, blocks_for(tokens, 2 * c.heads, g, steps, c.format == PQ_KV_INT8 ? 5 : 4), 256, 0, st, c, tokens, seq, pos, K_out, V_out, steps);
 }
 
 }  // namespace pq

@@ -6,6 +6,7 @@
 // Bound by memory: a row stays in the registers of the warps that own it from its load to its store, so that every tensor moves
 // once.
 #include <algorithm>
+#include <mutex>
 
 #include "pq_kernels.cuh"
 
@@ -13,124 +14,223 @@ namespace pq {
 
 constexpr int kNormSmemLimit = 224 * 1024;
 
-__device__ __forceinline__ void unpack8(const uint4& u, float (&v)[8]) {
+// Pairs of fp32 numbers: one instruction multiplies and adds two of them (a third of the instructions of these kernels, which at a bf16 value
+// a tensor and element are close to being bound by them)
+struct F2 { uint64_t v; };
+__device__ __forceinline__ F2 f2(float lo, float hi) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi)); return r; }
+__device__ __forceinline__ F2 f2(float x) { return f2(x, x); }
+__device__ __forceinline__ void get(const F2& a, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a.v)); }
+__device__ __forceinline__ F2 operator*(const F2& a, const F2& b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 operator+(const F2& a, const F2& b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 fma2(const F2& a, const F2& b, const F2& c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ float both(const F2& a) { float x, y; get(a, x, y); return x + y; }
+
+__device__ __forceinline__ void unpack8(const uint4& u, F2 (&v)[4]) {
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { v[2 * i] = bf16lo(w[i]); v[2 * i + 1] = bf16hi(w[i]); }
+  for (int i = 0; i < 4; ++i) v[i] = f2(bf16lo(w[i]), bf16hi(w[i]));
 }
-__device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
-  return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+__device__ __forceinline__ uint4 pack8(const F2 (&v)[4]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float x, y;
+    get(v[i], x, y);
+    w[i] = pack_bf16x2(x, y);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// gains and gates, which every row reads again: through L1
-__device__ __forceinline__ uint4 ldca8(const uint16_t* p, int chunk) { return __ldca(reinterpret_cast<const uint4*>(p) + chunk); }
 __device__ __forceinline__ uint4 ldcg8(const uint16_t* p, int chunk) { return __ldcg(reinterpret_cast<const uint4*>(p) + chunk); }
-__device__ __forceinline__ void ldca_f8(const float* p, int chunk, float (&v)[8]) {
-  const float4 a = __ldca(reinterpret_cast<const float4*>(p) + 2 * chunk), b = __ldca(reinterpret_cast<const float4*>(p) + 2 * chunk + 1);
-  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+__device__ __forceinline__ void ldcg_f8(const float* p, int chunk, F2 (&v)[4]) {
+  const float4 a = __ldcg(reinterpret_cast<const float4*>(p) + 2 * chunk), b = __ldcg(reinterpret_cast<const float4*>(p) + 2 * chunk + 1);
+  v[0] = f2(a.x, a.y); v[1] = f2(a.z, a.w); v[2] = f2(b.x, b.y); v[3] = f2(b.z, b.w);
 }
+template <int N>
+__device__ __forceinline__ void norm_copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void norm_copy_wait(int pending) {
+  switch (pending) {
+    case 0: norm_copy_wait<0>(); break;
+    case 1: norm_copy_wait<1>(); break;
+    case 2: norm_copy_wait<2>(); break;
+    default: norm_copy_wait<3>(); break;
+  }
+}
+
+// Rows of up to four tensors on their way through shared memory by asynchronous copies, [stage][tensor][piece][thread]: a thread copies what it
+// will read itself, so that nothing has to be waited for but its own copies.  Pieces behind the row's end and absent tensors
+// stay zero.
+template <int K, int CH, int RB>
+struct RowRing {
+  uint4* base;               // this thread's column of its team's part
+  const uint16_t* from[K];
+  long long ahead, step;
+  int lanes, l, chunks, N, T, stages, stage, into;      // stages: as many rows as are worked on at once (RB), and those on their way
+  __device__ uint4* place(int s, int k, int i) const { return base + (size_t)((s * K + k) * CH + i) * lanes; }
+  __device__ void begin() {
+    for (int s = 0; s < stages; ++s)
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+          if (!from[k] || l + i * lanes >= chunks) *place(s, k, i) = make_uint4(0, 0, 0, 0);
+    stage = 0;
+    into = stages - RB;
+    for (int s = 0; s < stages - RB; ++s) issue(s);
+  }
+  __device__ void issue(int s) {
+    if (ahead < T) {
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+          if (from[k] && l + i * lanes < chunks) cp_async16(smem_u32(place(s, k, i)), from[k] + ahead * N + (l + i * lanes) * 8, true);
+    }
+    ahead += step;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  __device__ int after(int s) const { return s + 1 == stages ? 0 : s + 1; }
+  __device__ void next() {                                     // the RB rows to work on are there, those behind them on their way
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+      issue(into);
+      into = after(into);
+    }
+    norm_copy_wait(stages - RB);
+  }
+  __device__ uint4 get(int b, int k, int i) const { return *place(b == 0 ? stage : after(stage), k, i); }
+  __device__ void done() {
+#pragma unroll
+    for (int b = 0; b < RB; ++b) stage = after(stage);
+  }
+};
 
 // Sums over the `warps` warps of a row's owners (a named barrier of theirs where a block holds several rows): every lane gets
 // them.  `slot` alternates between the two halves of `part`, so that one barrier a sum is enough.
 struct RowTeam {
-  float* part;               // [2][32][4] floats of this team in shared memory
+  float* part;               // [2][warps][8] floats of this team in shared memory
   int warps, warp, bar, slot;
-  __device__ void sum(float& a) { float b = 0.f, c = 0.f; sum(a, b, c); }
-  __device__ void sum(float& a, float& b, float& c) {
+  template <int K>
+  __device__ void sum(float (&v)[K]) {
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-      a += __shfl_xor_sync(0xffffffffu, a, d);
-      b += __shfl_xor_sync(0xffffffffu, b, d);
-      c += __shfl_xor_sync(0xffffffffu, c, d);
-    }
+    for (int d = 16; d > 0; d >>= 1)
+#pragma unroll
+      for (int k = 0; k < K; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], d);
     if (warps == 1) return;
-    float4* p = reinterpret_cast<float4*>(part) + slot * 32;
+    float4* p = reinterpret_cast<float4*>(part) + slot * 2 * warps;
     slot ^= 1;
-    if ((threadIdx.x & 31) == 0) p[warp] = make_float4(a, b, c, 0.f);
+    if ((threadIdx.x & 31) == 0) {
+      p[2 * warp] = make_float4(v[0], K > 1 ? v[K > 1 ? 1 : 0] : 0.f, K > 2 ? v[K > 2 ? 2 : 0] : 0.f, K > 3 ? v[K > 3 ? 3 : 0] : 0.f);
+      if (K > 4) p[2 * warp + 1] = make_float4(v[K > 4 ? 4 : 0], K > 5 ? v[K > 5 ? 5 : 0] : 0.f, 0.f, 0.f);
+    }
     asm volatile("bar.sync %0, %1;" ::"r"(bar), "r"(warps * 32) : "memory");
-    a = b = c = 0.f;
-    for (int w = 0; w < warps; ++w) { a += p[w].x; b += p[w].y; c += p[w].z; }
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] = 0.f;
+    for (int w = 0; w < warps; ++w) {
+      const float4 x = p[2 * w], y = K > 4 ? p[2 * w + 1] : make_float4(0, 0, 0, 0);
+      const float all[6] = {x.x, x.y, x.z, x.w, y.x, y.y};
+#pragma unroll
+      for (int k = 0; k < K; ++k) v[k] += all[k];
+    }
   }
 };
-constexpr int kTeamFloats = 2 * 32 * 4;
+__host__ __device__ constexpr int team_floats(int warps) { return 2 * 8 * warps; }
 
 // ---------------------------------------------------------------------------
-// k_block_norm: `warps` warps per row, CH pieces of 8 values per lane
+// k_block_norm: `warps` warps per row, CH pieces of 8 values per thread; teams of warps walk the rows with a stride.  The gains of a
+// thread's columns stay in its registers.
 // ---------------------------------------------------------------------------
-template <int CH>
-__global__ void __launch_bounds__(CH == 4 ? 512 : 1024) k_block_norm(const __grid_constant__ BlockNormArgs a, int warps) {
+template <int CH, bool Y, bool POST>
+__global__ void __launch_bounds__(CH == 1 ? 1024 : 512) k_block_norm(const __grid_constant__ BlockNormArgs a, int warps, int stages) {
   extern __shared__ float smem_f[];
   pdl_launch_dependents();
-  pdl_wait();
-  const int tid = threadIdx.x, lanes = warps * 32, team = tid / lanes, l = tid - team * lanes;
-  const long long row = (long long)blockIdx.x * (blockDim.x / lanes) + team;
-  if (row >= a.T) return;                       // a whole team: its barrier is its own
-  RowTeam rt{smem_f + team * kTeamFloats, warps, l >> 5, 1 + team, 0};
+  constexpr int K = Y ? 2 : 1;
+  const int tid = threadIdx.x, lanes = warps * 32, teams = blockDim.x / lanes, team = tid / lanes, l = tid - team * lanes;
+  RowTeam rt{smem_f + team * team_floats(warps), warps, l >> 5, 1 + team, 0};
   const int chunks = a.N / 8;
-  uint4 xr[CH], yr[CH];
+  long long row = (long long)blockIdx.x * teams + team;
+  const long long step = (long long)gridDim.x * teams;
+  RowRing<K, CH, 1> ring;
+  ring.base = reinterpret_cast<uint4*>(smem_f + teams * team_floats(warps)) + (size_t)team * stages * K * CH * lanes + l;
+  ring.from[0] = a.x;
+  if (Y) ring.from[K - 1] = a.y;
+  ring.ahead = row; ring.step = step;
+  ring.lanes = lanes; ring.l = l; ring.chunks = chunks; ring.N = a.N; ring.T = a.T; ring.stages = stages;
+  pdl_wait();
+  ring.begin();
+  const float gate1 = a.gate && !a.gate_vector ? __ldcg(a.gate) : 1.f, inv_n = 1.f / a.N;
+  uint4 pre[CH], post[POST ? CH : 1];
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
     const int c = l + i * lanes;
-    xr[i] = yr[i] = make_uint4(0, 0, 0, 0);
-    if (c < chunks) {
-      xr[i] = ldcg8(a.x + row * a.N, c);
-      if (a.y) yr[i] = ldcg8(a.y + row * a.N, c);
-    }
+    pre[i] = a.h && c < chunks ? ldcg8(a.pre, c) : make_uint4(0, 0, 0, 0);
+    if (POST) post[POST ? i : 0] = c < chunks ? ldcg8(a.post, c) : make_uint4(0, 0, 0, 0);
   }
-  float ry = 1.f;
-  if (a.post) {
-    float sq = 0.f;
+  for (; row < a.T; row += step) {
+    ring.next();
+    float ry = 1.f;
+    if (POST) {
+      F2 sq = f2(0.f);
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        F2 y[4];
+        unpack8(ring.get(0, K - 1, i), y);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sq = fma2(y[k], y[k], sq);
+      }
+      float v[1] = {both(sq)};
+      rt.sum(v);
+      ry = rsqrtf(v[0] * inv_n + a.eps);
+    }
+    const F2 by = f2(gate1 * ry), scale = f2(a.res_scale);
+    F2 s[CH][4], sq = f2(0.f);
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      float v[8];
-      unpack8(yr[i], v);
+      const int c = l + i * lanes;
+      unpack8(ring.get(0, 0, i), s[i]);
+      F2 u[4];
+      if (Y) {
+        unpack8(ring.get(0, K - 1, i), u);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) sq += v[k] * v[k];
-    }
-    rt.sum(sq);
-    ry = rsqrtf(sq / a.N + a.eps);
-  }
-  float s[CH][8], sq = 0.f;
-  const float gate1 = a.gate && !a.gate_vector ? __ldcg(a.gate) : 1.f;
+        for (int k = 0; k < 4; ++k) u[k] = u[k] * by;
+        if (POST) {
+          F2 w[4];
+          unpack8(post[POST ? i : 0], w);
 #pragma unroll
-  for (int i = 0; i < CH; ++i) {
-    const int c = l + i * lanes;
-    float u[8];
-    unpack8(xr[i], s[i]);
-    unpack8(yr[i], u);
-    if (c < chunks) {
-      if (a.post) {
-        float w[8];
-        unpack8(ldca8(a.post, c), w);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) u[k] = u[k] * ry * w[k];
+          for (int k = 0; k < 4; ++k) u[k] = u[k] * w[k];
+        }
+        if (a.gate_vector && c < chunks) {                     // 32 bytes a piece: read again, from L1
+          const float4 g0 = __ldca(reinterpret_cast<const float4*>(a.gate) + 2 * c), g1 = __ldca(reinterpret_cast<const float4*>(a.gate) + 2 * c + 1);
+          u[0] = u[0] * f2(g0.x, g0.y); u[1] = u[1] * f2(g0.z, g0.w); u[2] = u[2] * f2(g1.x, g1.y); u[3] = u[3] * f2(g1.z, g1.w);
+        }
       }
-      if (a.gate_vector) {
-        float w[8];
-        ldca_f8(a.gate, c, w);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) u[k] *= w[k];
+      for (int k = 0; k < 4; ++k) {
+        s[i][k] = Y ? fma2(scale, s[i][k], u[k]) : scale * s[i][k];
+        sq = fma2(s[i][k], s[i][k], sq);
       }
+      if (a.x_out && c < chunks) reinterpret_cast<uint4*>(a.x_out + row * a.N)[c] = pack8(s[i]);
     }
+    ring.done();
+    if (!a.h) continue;
+    float v[1] = {both(sq)};
+    rt.sum(v);
+    const F2 r = f2(rsqrtf(v[0] * inv_n + a.eps));
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      s[i][k] = a.res_scale * s[i][k] + gate1 * u[k];
-      sq += s[i][k] * s[i][k];
+    for (int i = 0; i < CH; ++i) {
+      const int c = l + i * lanes;
+      if (c >= chunks) continue;
+      F2 w[4];
+      unpack8(pre[i], w);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] = s[i][k] * r * w[k];
+      reinterpret_cast<uint4*>(a.h + row * a.N)[c] = pack8(w);
     }
-    if (a.x_out && c < chunks) reinterpret_cast<uint4*>(a.x_out + row * a.N)[c] = pack8(s[i]);
   }
-  if (!a.h) return;
-  rt.sum(sq);
-  const float r = rsqrtf(sq / a.N + a.eps);
-#pragma unroll
-  for (int i = 0; i < CH; ++i) {
-    const int c = l + i * lanes;
-    if (c >= chunks) continue;
-    float w[8];
-    unpack8(ldca8(a.pre, c), w);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) w[k] = s[i][k] * r * w[k];
-    reinterpret_cast<uint4*>(a.h + row * a.N)[c] = pack8(w);
-  }
+  norm_copy_wait<0>();
 }
 
 // ---------------------------------------------------------------------------
@@ -141,156 +241,159 @@ __global__ void __launch_bounds__(CH == 4 ? 512 : 1024) k_block_norm(const __gri
 // its columns for the whole launch, so that the sums over tokens stay in its registers; teams of a block meet in shared memory and
 // blocks in k_norm_sums, in a fixed order.
 // ---------------------------------------------------------------------------
-template <int N>
-__device__ __forceinline__ void norm_copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 template <int CH, bool POST, int GATE>     // GATE: 0 none, 1 one number, 2 per feature
 __global__ void __launch_bounds__(512, 1) k_block_norm_backward(const __grid_constant__ BlockNormArgs a, int warps, int stages, float* part, double* gate_part) {
   extern __shared__ float smem_f[];
   __shared__ double gate_sums[32];
   pdl_launch_dependents();
-  pdl_wait();
   constexpr bool kY = POST || GATE > 0;
-  constexpr int kTensors = kY ? 4 : 3;
+  constexpr int K = kY ? 4 : 3;
   const int tid = threadIdx.x, lanes = warps * 32, teams = blockDim.x / lanes, team = tid / lanes, l = tid - team * lanes;
-  RowTeam rt{smem_f + team * kTeamFloats, warps, l >> 5, 1 + team, 0};
+  RowTeam rt{smem_f + team * team_floats(warps), warps, l >> 5, 1 + team, 0};
   const int chunks = a.N / 8;
+  const long long step = (long long)gridDim.x * teams;
+  long long row = (long long)blockIdx.x * teams + team;
+  constexpr int RB = CH == 4 ? 1 : 2;                          // rows worked on at once: their sums meet in the same barriers
+  RowRing<K, CH, RB> ring;
+  ring.base = reinterpret_cast<uint4*>(smem_f + teams * team_floats(warps)) + (size_t)team * stages * K * CH * lanes + l;
+  ring.from[0] = a.dh ? a.x : nullptr;
+  ring.from[1] = a.dh;
+  ring.from[2] = a.dx_out;
+  if (kY) ring.from[K - 1] = a.y;
+  ring.ahead = row; ring.step = step;
+  ring.lanes = lanes; ring.l = l; ring.chunks = chunks; ring.N = a.N; ring.T = a.T; ring.stages = stages;
+  pdl_wait();
+  ring.begin();
   const float gate1 = GATE == 1 ? __ldcg(a.gate) : 1.f, inv_n = 1.f / a.N;
-  float spre[CH][8] = {}, sgate[GATE == 2 ? CH : 1][8] = {}, spost[POST ? CH : 1][8] = {};
+  const F2 zero = f2(0.f);
+  F2 spre[CH][4], sgate[GATE == 2 ? CH : 1][4], spost[POST ? CH : 1][4];
   double sgate1 = 0.0;
   // this thread's columns of the gains, zeros behind the row's end
   uint4 pre[CH], post[POST ? CH : 1];
-  float gate[GATE == 2 ? CH : 1][8];
+  F2 gate[GATE == 2 ? CH : 1][4];
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
     const int c = l + i * lanes;
     const bool ok = c < chunks;
     pre[i] = ok && a.dh ? ldcg8(a.pre, c) : make_uint4(0, 0, 0, 0);
     if (POST) post[POST ? i : 0] = ok ? ldcg8(a.post, c) : make_uint4(0, 0, 0, 0);
-    if (GATE == 2) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) gate[GATE == 2 ? i : 0][k] = 0.f;
-      if (ok) ldca_f8(a.gate, c, gate[GATE == 2 ? i : 0]);
+    for (int k = 0; k < 4; ++k) {
+      spre[i][k] = zero;
+      if (GATE == 2) sgate[GATE == 2 ? i : 0][k] = gate[GATE == 2 ? i : 0][k] = zero;
+      if (POST) spost[POST ? i : 0][k] = zero;
     }
+    if (GATE == 2 && ok) ldcg_f8(a.gate, c, gate[GATE == 2 ? i : 0]);
   }
-  // Rows come through a ring in shared memory by asynchronous copies, [stage][tensor][piece][thread]: a thread copies what it will read itself,
-  // so that nothing has to be waited for but its own copies.  Absent tensors and pieces behind the row's end stay zero.
-  uint4* const ring = reinterpret_cast<uint4*>(smem_f + teams * kTeamFloats) + (size_t)team * stages * kTensors * CH * lanes + l;
-  const uint16_t* const from[4] = {a.dh ? a.x : nullptr, a.dh, a.dx_out, kY ? a.y : nullptr};
-  auto place = [&](int stage, int tensor, int i) { return ring + (size_t)((stage * kTensors + tensor) * CH + i) * lanes; };
-  for (int s = 0; s < stages; ++s)
+  for (; row < a.T; row += RB * step) {
+    ring.next();
+    float sums[3 * RB];                                        // of each row: s^2, dh pre s, y^2
 #pragma unroll
-    for (int k = 0; k < kTensors; ++k)
+    for (int rb = 0; rb < RB; ++rb) {
+      F2 sq = zero, dot = zero, ysq = zero;
 #pragma unroll
-      for (int i = 0; i < CH; ++i)
-        if (!from[k] || l + i * lanes >= chunks) *place(s, k, i) = make_uint4(0, 0, 0, 0);
-  const long long step = (long long)gridDim.x * teams;
-  long long row = (long long)blockIdx.x * teams + team, ahead = row;
-  auto issue = [&](int stage) {
-    if (ahead < a.T) {
+      for (int i = 0; i < CH; ++i) {
+        F2 s[4], dh[4], w[4];
+        unpack8(ring.get(rb, 0, i), s);
+        unpack8(ring.get(rb, 1, i), dh);
+        unpack8(pre[i], w);
 #pragma unroll
-      for (int k = 0; k < kTensors; ++k)
+        for (int k = 0; k < 4; ++k) { sq = fma2(s[k], s[k], sq); dot = fma2(dh[k] * w[k], s[k], dot); }
+        if (POST) {
+          F2 y[4];
+          unpack8(ring.get(rb, K - 1, i), y);
 #pragma unroll
-        for (int i = 0; i < CH; ++i)
-          if (from[k] && l + i * lanes < chunks) cp_async16(smem_u32(place(stage, k, i)), from[k] + ahead * a.N + (l + i * lanes) * 8, true);
-    }
-    ahead += step;
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-  for (int s = 0; s < stages - 1; ++s) issue(s);
-  int stage = 0, into = stages - 1;
-  for (; row < a.T; row += step) {
-    issue(into);                                               // where the row before this one was
-    switch (stages) {
-      case 1: norm_copy_wait<0>(); break;
-      case 2: norm_copy_wait<1>(); break;
-      case 3: norm_copy_wait<2>(); break;
-      default: norm_copy_wait<3>(); break;
-    }
-    float sq = 0.f, dot = 0.f, ysq = 0.f;
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      float s[8], dh[8], w[8];
-      unpack8(*place(stage, 0, i), s);
-      unpack8(*place(stage, 1, i), dh);
-      unpack8(pre[i], w);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) { sq += s[k] * s[k]; dot += dh[k] * w[k] * s[k]; }
-      if (POST) {
-        float y[8];
-        unpack8(*place(stage, 3, i), y);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) ysq += y[k] * y[k];
-      }
-    }
-    rt.sum(sq, dot, ysq);
-    const float r = rsqrtf(sq * inv_n + a.eps), corr = dot * inv_n * r * r, ry = POST ? rsqrtf(ysq * inv_n + a.eps) : 1.f;
-    float e[CH][8], edot = 0.f;
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const int c = l + i * lanes;
-      float s[8], dh[8], w[8], g[8];
-      unpack8(*place(stage, 0, i), s);
-      unpack8(*place(stage, 1, i), dh);
-      unpack8(*place(stage, 2, i), g);
-      unpack8(pre[i], w);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        spre[i][k] += dh[k] * (s[k] * r);
-        g[k] += r * (dh[k] * w[k] - s[k] * corr);
-      }
-      if (c < chunks) {
-        float dx[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) dx[k] = a.res_scale * g[k];
-        reinterpret_cast<uint4*>(a.dx + row * a.N)[c] = pack8(dx);
-      }
-      if (kY) {
-        float y[8], pw[8];
-        unpack8(*place(stage, kTensors - 1, i), y);
-        if (POST) unpack8(post[POST ? i : 0], pw);
-        float line = 0.f;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float m = y[k] * ry, u = POST ? m * pw[k] : m;
-          if (GATE == 2) sgate[GATE == 2 ? i : 0][k] += g[k] * u;
-          if (GATE == 1) line += g[k] * u;
-          const float ge = g[k] * (GATE == 2 ? gate[GATE == 2 ? i : 0][k] : gate1);
-          if (POST) {
-            spost[POST ? i : 0][k] += ge * m;
-            e[i][k] = ge * pw[k];
-            edot += e[i][k] * m;
-          } else {
-            e[i][k] = ge;
-          }
+          for (int k = 0; k < 4; ++k) ysq = fma2(y[k], y[k], ysq);
         }
-        if (GATE == 1) sgate1 += (double)line;
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) e[i][k] = g[k];
       }
+      sums[3 * rb] = both(sq);
+      sums[3 * rb + 1] = both(dot);
+      sums[3 * rb + 2] = POST ? both(ysq) : 0.f;
     }
-    if (a.dy) {
-      if (POST) { rt.sum(edot); edot *= inv_n; }
+    rt.sum(sums);
+    F2 e[RB][CH][4], ry2[RB];
+    float edot[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const long long here = row + rb * step;
+      edot[rb] = 0.f;
+      if (here >= a.T) break;                                  // the ring still holds an older row there
+      const float r = rsqrtf(sums[3 * rb] * inv_n + a.eps), ry = POST ? rsqrtf(sums[3 * rb + 2] * inv_n + a.eps) : 1.f;
+      const F2 r2 = f2(r), corr = f2(-sums[3 * rb + 1] * inv_n * r * r), scale = f2(a.res_scale), g1 = f2(gate1);
+      ry2[rb] = f2(ry);
+      F2 edot2 = zero;
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
         const int c = l + i * lanes;
-        if (c >= chunks) continue;
-        if (POST) {
-          float y[8];
-          unpack8(*place(stage, kTensors - 1, i), y);
+        F2 s[4], dh[4], w[4], g[4];
+        unpack8(ring.get(rb, 0, i), s);
+        unpack8(ring.get(rb, 1, i), dh);
+        unpack8(ring.get(rb, 2, i), g);
+        unpack8(pre[i], w);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) e[i][k] = ry * (e[i][k] - y[k] * ry * edot);
+        for (int k = 0; k < 4; ++k) {
+          spre[i][k] = fma2(dh[k], s[k] * r2, spre[i][k]);
+          g[k] = fma2(r2, fma2(s[k], corr, dh[k] * w[k]), g[k]);
         }
-        reinterpret_cast<uint4*>(a.dy + row * a.N)[c] = pack8(e[i]);
+        if (c < chunks) {
+          F2 dx[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) dx[k] = scale * g[k];
+          reinterpret_cast<uint4*>(a.dx + here * a.N)[c] = pack8(dx);
+        }
+        if (kY) {
+          F2 y[4], pw[4], line = zero;
+          unpack8(ring.get(rb, K - 1, i), y);
+          if (POST) unpack8(post[POST ? i : 0], pw);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const F2 m = POST ? y[k] * ry2[rb] : y[k], u = POST ? m * pw[k] : m;
+            if (GATE == 2) sgate[GATE == 2 ? i : 0][k] = fma2(g[k], u, sgate[GATE == 2 ? i : 0][k]);
+            if (GATE == 1) line = fma2(g[k], u, line);
+            const F2 ge = GATE == 2 ? g[k] * gate[GATE == 2 ? i : 0][k] : GATE == 1 ? g[k] * g1 : g[k];
+            if (POST) {
+              spost[POST ? i : 0][k] = fma2(ge, m, spost[POST ? i : 0][k]);
+              e[rb][i][k] = ge * pw[k];
+              edot2 = fma2(e[rb][i][k], m, edot2);
+            } else {
+              e[rb][i][k] = ge;
+            }
+          }
+          if (GATE == 1) sgate1 += (double)both(line);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) e[rb][i][k] = g[k];
+        }
+        if (!POST && a.dy && c < chunks) reinterpret_cast<uint4*>(a.dy + here * a.N)[c] = pack8(e[rb][i]);
+      }
+      edot[rb] = both(edot2);
+    }
+    if (POST) {
+      rt.sum(edot);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const long long here = row + rb * step;
+        if (here >= a.T) break;
+        float ry, ry_;
+        get(ry2[rb], ry, ry_);
+        const F2 take = f2(-edot[rb] * inv_n * ry);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+          const int c = l + i * lanes;
+          if (c >= chunks) continue;
+          F2 y[4];
+          unpack8(ring.get(rb, K - 1, i), y);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) e[rb][i][k] = ry2[rb] * fma2(y[k], take, e[rb][i][k]);
+          reinterpret_cast<uint4*>(a.dy + here * a.N)[c] = pack8(e[rb][i]);
+        }
       }
     }
-    stage = stage + 1 == stages ? 0 : stage + 1;
-    into = into + 1 == stages ? 0 : into + 1;
+    ring.done();
   }
   norm_copy_wait<0>();
   // ---- the block's sums: teams one after another into shared memory (the rings are free), [dpre, dgate, dpost][N]
-  float* acc = smem_f + teams * kTeamFloats;
+  float* acc = smem_f + teams * team_floats(warps);
   const int n = a.N;
   for (int turn = 0; turn < teams; ++turn) {
     __syncthreads();
@@ -300,11 +403,17 @@ __global__ void __launch_bounds__(512, 1) k_block_norm_backward(const __grid_con
       const int c = l + i * lanes;
       if (c >= chunks) continue;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        float* p = acc + c * 8 + k;
-        p[0] = spre[i][k] + (turn ? p[0] : 0.f);
-        if (GATE == 2) p[n] = sgate[GATE == 2 ? i : 0][k] + (turn ? p[n] : 0.f);
-        if (POST) p[(GATE == 2 ? 2 : 1) * n] = spost[POST ? i : 0][k] + (turn ? p[(GATE == 2 ? 2 : 1) * n] : 0.f);
+      for (int k = 0; k < 4; ++k) {
+        auto put = [&](float* p, const F2& v) {
+          float x, y;
+          get(v, x, y);
+          p[0] = x + (turn ? p[0] : 0.f);
+          p[1] = y + (turn ? p[1] : 0.f);
+        };
+        float* p = acc + c * 8 + 2 * k;
+        put(p, spre[i][k]);
+        if (GATE == 2) put(p + n, sgate[GATE == 2 ? i : 0][k]);
+        if (POST) put(p + (GATE == 2 ? 2 : 1) * n, spost[POST ? i : 0][k]);
       }
     }
   }
@@ -362,26 +471,58 @@ __global__ void __launch_bounds__(256) k_norm_sums(const float* part, int blocks
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
+// The opt-in limits, once per device
+template <int CH>
+static auto norm_kernel(bool y, bool post) { return post ? k_block_norm<CH, true, true> : y ? k_block_norm<CH, true, false> : k_block_norm<CH, false, false>; }
+template <int CH>
+static auto norm_bwd_kernel(bool post, int gate) {
+  return post ? (gate == 0 ? k_block_norm_backward<CH, true, 0> : gate == 1 ? k_block_norm_backward<CH, true, 1> : k_block_norm_backward<CH, true, 2>)
+              : (gate == 0 ? k_block_norm_backward<CH, false, 0> : gate == 1 ? k_block_norm_backward<CH, false, 1> : k_block_norm_backward<CH, false, 2>);
+}
+static cudaError_t norm_limits() {
+  constexpr int kMaxDevices = 64;
+  static std::once_flag done[kMaxDevices];
+  static cudaError_t result[kMaxDevices] = {};
+  int dev = 0;
+  if (const cudaError_t e = cudaGetDevice(&dev)) return e;
+  if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+  std::call_once(done[dev], [&] {
+    auto set = [&](auto k) { if (result[dev] == cudaSuccess) result[dev] = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kNormSmemLimit); };
+    for (int post = 0; post < 2; ++post) {
+      for (int y = post; y < 2; ++y) { set(norm_kernel<1>(y, post)); set(norm_kernel<4>(y, post)); }
+      for (int gate = 0; gate < 3; ++gate) { set(norm_bwd_kernel<1>(post, gate)); set(norm_bwd_kernel<2>(post, gate)); set(norm_bwd_kernel<4>(post, gate)); }
+    }
+  });
+  return result[dev];
+}
+// as many rows in flight as fit, four at most
+static int norm_stages(size_t row_bytes, size_t fixed, int least, int most) {
+  return (int)std::max<size_t>(least, std::min<size_t>(most, (kNormSmemLimit - fixed) / row_bytes));
+}
+
 cudaError_t launch_block_norm_forward(const BlockNormArgs& a, cudaStream_t st) {
-  const int chunks = a.N / 8;
-  // few rows: a lane per piece, the row's latency; many: four pieces a lane
-  const int ch = a.T <= 2 * sm_count() ? 1 : 4;
-  int warps = 1;
-  while (warps < 32 && warps * 32 * ch < chunks) warps *= 2;
-  const int use = warps * 32 >= chunks ? 1 : warps * 64 >= chunks ? 2 : 4;
-  auto kern = use == 1 ? k_block_norm<1> : use == 2 ? k_block_norm<2> : k_block_norm<4>;
-  const int rows = std::max(1, 8 / warps);
+  if (const cudaError_t e = norm_limits()) return e;
+  const int chunks = a.N / 8, tensors = a.y ? 2 : 1;
+  // few rows: a thread per piece, the row's latency; many: four pieces a thread, fewer warps to meet per row and more rows at work
+  const int ch = chunks <= 1024 && a.T <= sm_count() ? 1 : 4, most = ch == 1 ? 32 : 16;
+  const int warps = (chunks + 32 * ch - 1) / (32 * ch);
+  const int teams = std::max(1, std::min(most / warps, 15));                                  // named barriers
+  const int blocks = std::min((a.T + teams - 1) / teams, sm_count());
+  const bool few = a.T <= blocks * teams;                                                     // one row a team: nothing behind it
+  const size_t fixed = (size_t)teams * team_floats(warps) * sizeof(float), row = (size_t)tensors * ch * warps * 32 * 16 * teams;
+  const int stages = norm_stages(row, fixed, 1, few ? 1 : 4);
+  auto kern = ch == 1 ? norm_kernel<1>(a.y != nullptr, a.post != nullptr) : norm_kernel<4>(a.y != nullptr, a.post != nullptr);
   LaunchScope ls(KID_NORM_FWD, st);
-  return launch_pdl(kern, (a.T + rows - 1) / rows, rows * warps * 32, rows * kTeamFloats * sizeof(float), st, a, warps);
+  return launch_pdl(kern, blocks, teams * warps * 32, fixed + stages * row, st, a, warps, stages);
 }
 
 struct NormBwdPlan { int ch, warps, teams, blocks; };
 static NormBwdPlan norm_bwd_plan(int T, int N) {
   NormBwdPlan p{};
   const int chunks = N / 8;
-  p.ch = chunks <= 512 ? 1 : chunks <= 1024 ? 2 : 4;
+  p.ch = chunks <= 256 ? 1 : chunks <= 1024 ? 2 : 4;           // two rows at work in a block as long as they fit
   p.warps = (chunks + 32 * p.ch - 1) / (32 * p.ch);
-  p.teams = p.ch == 1 ? std::max(1, 16 / p.warps) : 1;
+  p.teams = std::max(1, std::min(16 / p.warps, 15));           // named barriers
   p.blocks = std::min(sm_count(), (T + p.teams - 1) / p.teams);
   return p;
 }
@@ -390,11 +531,6 @@ size_t block_norm_workspace_bytes(int T, int N) {
   return ((size_t)p.blocks * 3 * N * 4 + 255) / 256 * 256 + (size_t)p.blocks * 8;
 }
 
-template <int CH>
-static auto norm_bwd_kernel(bool post, int gate) {
-  return post ? (gate == 0 ? k_block_norm_backward<CH, true, 0> : gate == 1 ? k_block_norm_backward<CH, true, 1> : k_block_norm_backward<CH, true, 2>)
-              : (gate == 0 ? k_block_norm_backward<CH, false, 0> : gate == 1 ? k_block_norm_backward<CH, false, 1> : k_block_norm_backward<CH, false, 2>);
-}
 cudaError_t launch_block_norm_backward(const BlockNormArgs& a, void* ws, cudaStream_t st) {
   const NormBwdPlan p = norm_bwd_plan(a.T, a.N);
   float* part = static_cast<float*>(ws);
@@ -402,11 +538,11 @@ cudaError_t launch_block_norm_backward(const BlockNormArgs& a, void* ws, cudaStr
   const int gate = !a.gate ? 0 : a.gate_vector ? 2 : 1, sums = 1 + (gate == 2) + (a.post != nullptr);
   const bool post = a.post != nullptr;
   auto kern = p.ch == 1 ? norm_bwd_kernel<1>(post, gate) : p.ch == 2 ? norm_bwd_kernel<2>(post, gate) : norm_bwd_kernel<4>(post, gate);
-  // as many rows in flight as fit, four at most; the sums over tokens take the ring's place in the end
-  const size_t row = (size_t)(a.post || a.gate ? 4 : 3) * p.ch * p.warps * 32 * 16 * p.teams, fixed = (size_t)p.teams * kTeamFloats * sizeof(float);
-  const int stages = (int)std::max<size_t>(1, std::min<size_t>(4, (kNormSmemLimit - fixed) / row));
+  if (const cudaError_t e = norm_limits()) return e;
+  // the sums over tokens take the ring's place in the end
+  const size_t row = (size_t)(a.post || a.gate ? 4 : 3) * p.ch * p.warps * 32 * 16 * p.teams, fixed = (size_t)p.teams * team_floats(p.warps) * sizeof(float);
+  const int stages = norm_stages(row, fixed, p.ch == 4 ? 1 : 2, 4);
   const size_t smem = fixed + std::max(stages * row, (size_t)sums * a.N * sizeof(float));
-  if (const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kNormSmemLimit)) return e;
   {
     LaunchScope ls(KID_NORM_BWD, st);
     if (const cudaError_t e = launch_pdl(kern, p.blocks, p.teams * p.warps * 32, smem, st, a, p.warps, stages, part, gate_part)) return e;

@@ -230,7 +230,17 @@ def test_binding_checks_types_shapes_and_layouts(lib):
             lib.make_kv_cache(a["K"], a["V"], a["table"], 100, a["kg"])
     c = lib.make_kv_cache(t(8, 4, 32, 104), t(8, 4, 32, 104), table, 100)
     assert (c.heads, c.head_dim, c.page_size, c.num_pages, c.num_seqs, c.max_pages) == (4, 100, 32, 8, 3, 5)
-    assert lib._rows("f", "x", t(5, 64), 5, 64) == 64 and lib._rows("f", "x", t(5, 96)[:, 32:], 5, 64) == 96 and lib._rows("f", "x", t(5, 2, 32), 5, 64) == 0
-    for bad in (t(5, 64, dtype=torch.float16), t(64, 5).t(), t(4, 64), t(5, 2, 64)[:, :, :32]):
+    # rows: dense or with a stride; on another device than the current one they are refused (here: the CPU, device -1)
+    assert lib._rows_at("f", "x", t(5, 64), 5, 64, -1)[1] == 0 and lib._rows_at("f", "x", t(5, 2, 32), 5, 64, -1)[1] == 0
+    assert lib._rows_at("f", "x", t(5, 96)[:, 32:], 5, 64, -1)[1] == 96 and lib._rows_at("f", "x", t(1, 96)[:, 32:], 1, 64, -1)[1] == 0
+    for bad in (t(5, 64, dtype=torch.float16), t(64, 5).t(), t(4, 64), t(5, 2, 64)[:, :, :32], t(5, 128)[:, ::2]):
         with pytest.raises(lib.PqArgumentError):
-            lib._rows("f", "x", bad, 5, 64)
+            lib._rows_at("f", "x", bad, 5, 64, -1)
+    for x in (t(5, 64), t(5, 96)[:, 32:]):
+        with pytest.raises(lib.PqArgumentError, match="current device"):
+            lib._rows_at("f", "x", x, 5, 64, 0)
+    with pytest.raises(lib.PqArgumentError, match="contiguous"):
+        lib._at("f", "x", t(64, 5).t(), torch.bfloat16, 320, -1)
+    with pytest.raises(lib.PqArgumentError):
+        lib._whole("f", "x", t(5, 64), 100)
+    assert lib._at("f", "x", None, torch.int32, 7, 0) is None
