@@ -5,8 +5,9 @@
 // sequence, page id and row are four trips to memory one after another; warps walk the units with a stride and ask for the next
 // unit's indices before they work on this one's rows.
 #include <algorithm>
+#include <cstring>
 
-#include "pq_kernels.cuh"
+#include "pq_pairs.cuh"
 
 namespace pq {
 
@@ -27,38 +28,44 @@ __device__ __forceinline__ long long kv_row(const KvCache& c, int2 place, int he
   return ((long long)place.x * c.heads + head) * c.page_size + place.y;
 }
 
-// rounded to the nearest integer (ties to even), saturated to -128 .. 127
-__device__ __forceinline__ int sat_s8(float x) {
-  int v;
-  asm("cvt.rni.sat.s8.f32 %0, %1;" : "=r"(v) : "f"(x));
-  return v;
-}
-// The loads of this file bypass L1: what an earlier kernel wrote must be seen by one that is resident already
+// VEC bf16 values as pairs.  The loads of this file bypass L1: what an earlier kernel wrote must be seen by one that is resident already.
+template <int W> struct Words;
+template <> struct Words<4> { using T = uint4; };
+template <> struct Words<2> { using T = uint2; };
+template <> struct Words<1> { using T = uint32_t; };
 template <int VEC>
-__device__ __forceinline__ void store_bf16(uint16_t* p, const float (&v)[VEC]) {
-  if constexpr (VEC == 8)
-    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
-  else if constexpr (VEC == 4)
-    *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-  else
-    *reinterpret_cast<uint32_t*>(p) = pack_bf16x2(v[0], v[1]);
+struct Bf {
+  uint32_t w[VEC / 2];
+  __device__ void load(const uint16_t* p) {
+    using T = typename Words<VEC / 2>::T;
+    const T v = __ldcg(reinterpret_cast<const T*>(p));
+    memcpy(w, &v, sizeof v);
+  }
+  __device__ void store(uint16_t* p) const {
+    using T = typename Words<VEC / 2>::T;
+    T v;
+    memcpy(&v, w, sizeof v);
+    *reinterpret_cast<T*>(p) = v;
+  }
+  __device__ F2 pair(int k) const { return f2(bf16lo(w[k]), bf16hi(w[k])); }
+};
+__device__ __forceinline__ uint32_t pack_pair(const F2& v) {
+  float x, y;
+  get(v, x, y);
+  return pack_bf16x2(x, y);
+}
+// Two values times gamma, rounded to integers (ties to even) and limited to 127, in the low bytes of the result: behind 1.5 x 2^23 a
+// number's last bits are the integer.  (Below -128 none can fall: |x| gamma <= 128.)
+__device__ __forceinline__ void code_pair(const F2& x, const F2& gamma, uint32_t& lo, uint32_t& hi) {
+  float a, b;
+  get(x * gamma, a, b);
+  const F2 r = f2(fminf(a, 127.f), fminf(b, 127.f)) + f2(12582912.f);
+  get(r, a, b);
+  lo = __float_as_uint(a);
+  hi = __float_as_uint(b);
 }
 
 constexpr int kSteps = 4;        // of a unit at most; with few rows one, so that they spread over more warps
-
-// The raw bits of VEC bf16 values
-template <int VEC> struct Raw;
-template <> struct Raw<8> { uint4 v; };
-template <> struct Raw<4> { uint2 v; };
-template <> struct Raw<2> { uint32_t v; };
-template <int VEC>
-__device__ __forceinline__ void load_raw(const uint16_t* p, Raw<VEC>& r) { r.v = __ldcg(reinterpret_cast<const decltype(r.v)*>(p)); }
-__device__ __forceinline__ void raw_floats(const Raw<8>& r, float (&v)[8]) {
-  const uint32_t w[4] = {r.v.x, r.v.y, r.v.z, r.v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { v[2 * i] = bf16lo(w[i]); v[2 * i + 1] = bf16hi(w[i]); }
-}
-__device__ __forceinline__ void raw_floats(const Raw<2>& r, float (&v)[2]) { v[0] = bf16lo(r.v); v[1] = bf16hi(r.v); }
 
 // A warp's walk over units = (token, rows of it).  While a unit is worked on, the place of the next one is looked up and the position and
 // sequence of the one behind it are on their way.
@@ -121,17 +128,17 @@ __global__ void __launch_bounds__(256, VEC == 8 ? 2 : 3) k_kv_append(KvCache c, 
     const uint16_t* const q_row = Q + tok * q_stride;
     const uint16_t* const k_row = K + tok * k_stride - (long long)q_heads * c.dim;                  // of row r: + r dim
     const uint16_t* const v_row = V + tok * v_stride - (long long)(q_heads + c.heads) * c.dim;
-    Raw<VEC> ra[kSteps][kMost], rb[kSteps][kMost];
+    Bf<VEC> ra[kSteps][kMost], rb[kSteps][kMost];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
       const int r = row0 + s * kRows;
       const uint16_t* src = (r < q_heads ? q_row : r < q_heads + c.heads ? k_row : v_row) + (long long)r * c.dim + lane * VEC;
 #pragma unroll
       for (int i = 0; i < kMost; ++i)
-        if (s < steps && r < rows && lane + i * G < pieces) { load_raw<VEC>(src + i * G * VEC, ra[s][i]); load_raw<VEC>(src + half + i * G * VEC, rb[s][i]); }
+        if (s < steps && r < rows && lane + i * G < pieces) { ra[s][i].load(src + i * G * VEC); rb[s][i].load(src + half + i * G * VEC); }
     }
     // other warps turn other rows of the token by the same angles: through L1
-    float cs[kMost][VEC], sn[kMost][VEC];
+    F2 cs[kMost][VEC / 2], sn[kMost][VEC / 2];
     const bool turns = cos_t && at >= 0 && at < rope_rows;
 #pragma unroll
     for (int i = 0; i < kMost; ++i) {
@@ -139,16 +146,17 @@ __global__ void __launch_bounds__(256, VEC == 8 ? 2 : 3) k_kv_append(KvCache c, 
       if (!turns || p >= pieces) continue;
       const float* cr = cos_t + (long long)at * half + p * VEC;
       const float* sr = sin_t + (long long)at * half + p * VEC;
-      if constexpr (VEC == 8) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const float4 x = __ldca(reinterpret_cast<const float4*>(cr) + k), y = __ldca(reinterpret_cast<const float4*>(sr) + k);
-          cs[i][4 * k] = x.x; cs[i][4 * k + 1] = x.y; cs[i][4 * k + 2] = x.z; cs[i][4 * k + 3] = x.w;
-          sn[i][4 * k] = y.x; sn[i][4 * k + 1] = y.y; sn[i][4 * k + 2] = y.z; sn[i][4 * k + 3] = y.w;
+      for (int k = 0; k < VEC / 2; k += 2) {
+        if constexpr (VEC == 8) {
+          const float4 x = __ldca(reinterpret_cast<const float4*>(cr) + k / 2), y = __ldca(reinterpret_cast<const float4*>(sr) + k / 2);
+          cs[i][k] = f2(x.x, x.y); cs[i][k + 1] = f2(x.z, x.w);
+          sn[i][k] = f2(y.x, y.y); sn[i][k + 1] = f2(y.z, y.w);
+        } else {
+          const float2 x = __ldca(reinterpret_cast<const float2*>(cr)), y = __ldca(reinterpret_cast<const float2*>(sr));
+          cs[i][0] = f2(x.x, x.y);
+          sn[i][0] = f2(y.x, y.y);
         }
-      } else {
-        const float2 x = __ldca(reinterpret_cast<const float2*>(cr)), y = __ldca(reinterpret_cast<const float2*>(sr));
-        cs[i][0] = x.x; cs[i][1] = x.y; sn[i][0] = y.x; sn[i][1] = y.y;
       }
     }
     more = w.more();
@@ -163,68 +171,62 @@ __global__ void __launch_bounds__(256, VEC == 8 ? 2 : 3) k_kv_append(KvCache c, 
       const int r = row0 + s * kRows;
       if (s >= steps || r >= rows) break;
       const bool query = r < q_heads, key = r < q_heads + c.heads;     // else a value
-      float a[kMost][VEC], b[kMost][VEC];
-      uint32_t amax = 0;
+      uint32_t amax = 0;                                               // of pairs: two 16-bit numbers
 #pragma unroll
       for (int i = 0; i < kMost; ++i) {
         if (lane + i * G >= pieces) continue;
-        raw_floats(ra[s][i], a[i]);
-        raw_floats(rb[s][i], b[i]);
         if (turns && key) {
+          // products and sums one by one (of pairs they came out fused, one rounding short)
 #pragma unroll
-          for (int k = 0; k < VEC; k += 2) {
-            float u[2], v[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              u[j] = __fsub_rn(__fmul_rn(a[i][k + j], cs[i][k + j]), __fmul_rn(b[i][k + j], sn[i][k + j]));
-              v[j] = __fadd_rn(__fmul_rn(b[i][k + j], cs[i][k + j]), __fmul_rn(a[i][k + j], sn[i][k + j]));
-            }
-            const uint32_t x = pack_bf16x2(u[0], u[1]), y = pack_bf16x2(v[0], v[1]);
-            a[i][k] = bf16lo(x); a[i][k + 1] = bf16hi(x);
-            b[i][k] = bf16lo(y); b[i][k + 1] = bf16hi(y);
+          for (int k = 0; k < VEC / 2; ++k) {
+            float c0, c1, s0, s1;
+            get(cs[i][k], c0, c1);
+            get(sn[i][k], s0, s1);
+            const float a0 = bf16lo(ra[s][i].w[k]), a1 = bf16hi(ra[s][i].w[k]), b0 = bf16lo(rb[s][i].w[k]), b1 = bf16hi(rb[s][i].w[k]);
+            ra[s][i].w[k] = pack_bf16x2(__fsub_rn(__fmul_rn(a0, c0), __fmul_rn(b0, s0)), __fsub_rn(__fmul_rn(a1, c1), __fmul_rn(b1, s1)));
+            rb[s][i].w[k] = pack_bf16x2(__fadd_rn(__fmul_rn(b0, c0), __fmul_rn(a0, s0)), __fadd_rn(__fmul_rn(b1, c1), __fmul_rn(a1, s1)));
           }
         }
         if (I8) {
 #pragma unroll
-          for (int k = 0; k < VEC; ++k)      // as integers: a NaN is above infinity is above the rest
-            amax = max(amax, max(__float_as_uint(a[i][k]) & 0x7fffffffu, __float_as_uint(b[i][k]) & 0x7fffffffu));
+          for (int k = 0; k < VEC / 2; ++k)      // bits of bf16 without the sign: a NaN is above infinity is above the rest
+            amax = __vmaxu2(amax, __vmaxu2(ra[s][i].w[k] & 0x7fff7fffu, rb[s][i].w[k] & 0x7fff7fffu));
         }
       }
       const int head = query ? r : key ? r - q_heads : r - q_heads - c.heads;
       if (query || !I8) {
         uint16_t* dst = query ? Q_out + ((long long)tok * q_heads + head) * c.dim : static_cast<uint16_t*>(key ? c.K : c.V) + crow0 * c.pitch + head * head_rows;
+        dst += lane * VEC;
 #pragma unroll
-        for (int i = 0; i < kMost; ++i) {
-          const int p = lane + i * G;
-          if (p < pieces) { store_bf16<VEC>(dst + p * VEC, a[i]); store_bf16<VEC>(dst + half + p * VEC, b[i]); }
-        }
-        if (!query && lane < c.pitch - c.dim) dst[c.dim + lane] = 0;      // at most 4 of them
+        for (int i = 0; i < kMost; ++i)
+          if (lane + i * G < pieces) { ra[s][i].store(dst + i * G * VEC); rb[s][i].store(dst + half + i * G * VEC); }
+        if (!query && lane < c.pitch - c.dim) dst[c.dim + lane - lane * VEC] = 0;      // at most 4 of them
         continue;
       }
+      amax = max(amax & 0xffffu, amax >> 16);
 #pragma unroll
       for (int d = G / 2; d > 0; d >>= 1) amax = max(amax, __shfl_xor_sync(mask, amax, d));
-      const bool finite = amax < 0x7f800000u;
-      const float gamma = finite ? __fdiv_rn(kActQmax, fmaxf(__uint_as_float(amax), kActAmaxFloor)) : __uint_as_float(0x7fffffffu);
+      const bool finite = amax < 0x7f80u;
+      const float gamma = finite ? __fdiv_rn(kActQmax, fmaxf(__uint_as_float(amax << 16), kActAmaxFloor)) : __uint_as_float(0x7fffffffu);
+      const F2 g2 = f2(gamma);
       int8_t* dst = static_cast<int8_t*>(key ? c.K : c.V) + crow0 * c.pitch + head * head_rows;
-      auto code = [&](float x) { return finite ? sat_s8(__fmul_rn(x, gamma)) & 0xff : 0; };
+      auto put = [&](int8_t* to, const Bf<VEC>& v) {
+        uint32_t b[VEC];
 #pragma unroll
-      for (int i = 0; i < kMost; ++i) {
-        const int p = lane + i * G;
-        if (p >= pieces) continue;
-        auto put = [&](int8_t* to, const float (&v)[VEC]) {
-          if constexpr (VEC == 8) {
-            uint2 x;
-            x.x = code(v[0]) | code(v[1]) << 8 | code(v[2]) << 16 | code(v[3]) << 24;
-            x.y = code(v[4]) | code(v[5]) << 8 | code(v[6]) << 16 | code(v[7]) << 24;
-            *reinterpret_cast<uint2*>(to) = x;
-          } else {
-            *reinterpret_cast<uint16_t*>(to) = (uint16_t)(code(v[0]) | code(v[1]) << 8);
-          }
-        };
-        put(dst + p * VEC, a[i]);
-        put(dst + half + p * VEC, b[i]);
-      }
-      for (int i = c.dim + lane; i < c.pitch; i += G) dst[i] = 0;
+        for (int k = 0; k < VEC / 2; ++k) code_pair(v.pair(k), g2, b[2 * k], b[2 * k + 1]);
+        if constexpr (VEC == 8) {
+          uint2 x;
+          x.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+          x.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
+          *reinterpret_cast<uint2*>(to) = finite ? x : make_uint2(0, 0);
+        } else {
+          *reinterpret_cast<uint16_t*>(to) = finite ? (uint16_t)__byte_perm(b[0], b[1], 0x0040) : (uint16_t)0;
+        }
+      };
+#pragma unroll
+      for (int i = 0; i < kMost; ++i)
+        if (lane + i * G < pieces) { put(dst + (lane + i * G) * VEC, ra[s][i]); put(dst + half + (lane + i * G) * VEC, rb[s][i]); }
+      if (lane < c.pitch - c.dim) dst[c.dim + lane] = 0;               // at most 12
       if (lane == 0) (key ? c.k_gamma : c.v_gamma)[crow0 + (long long)head * c.page_size] = gamma;
     }
   }
@@ -237,12 +239,12 @@ __global__ void __launch_bounds__(256, VEC == 8 ? 2 : 3) k_kv_append(KvCache c, 
 // more than the memory asks for.
 // ---------------------------------------------------------------------------
 template <int VEC, int G, bool I8>
-__global__ void __launch_bounds__(256, I8 ? 5 : 4) k_kv_read(KvCache c, int tokens, const int* seq, const int* pos, uint16_t* K_out, uint16_t* V_out, int steps) {
+__global__ void __launch_bounds__(256, 4) k_kv_read(KvCache c, int tokens, const int* seq, const int* pos, uint16_t* K_out, uint16_t* V_out, int steps) {
   pdl_launch_dependents();
   pdl_wait();
   constexpr int kMost = VEC == 8 ? 1 : 2;                              // pieces per lane (G = 16: head_dim <= 128)
   constexpr int kRows = 32 / G, kBytes = I8 ? 1 : 2;
-  using In = Raw<I8 ? VEC / 2 : VEC>;                                  // the bytes of VEC values
+  using In = Bf<I8 ? VEC / 2 : VEC>;                                   // the bytes of VEC values
   const int lane = threadIdx.x % G, sub = threadIdx.x % 32 / G, pieces = c.dim / VEC, rows = 2 * c.heads;
   const long long head_bytes = (long long)c.page_size * c.pitch * kBytes;
   KvWalk w;
@@ -266,7 +268,7 @@ __global__ void __launch_bounds__(256, I8 ? 5 : 4) k_kv_read(KvCache c, int toke
         const uint8_t* src = (r < c.heads ? k_src : v_src) + head * head_bytes;
 #pragma unroll
         for (int i = 0; i < kMost; ++i)
-          if (lane + i * G < pieces) raw[s][i].v = __ldcg(reinterpret_cast<const decltype(raw[s][i].v)*>(src + i * G * VEC * kBytes));
+          if (lane + i * G < pieces) raw[s][i].load(reinterpret_cast<const uint16_t*>(src + i * G * VEC * kBytes));
         if (I8) gamma[s] = __ldcg((r < c.heads ? c.k_gamma : c.v_gamma) + crow0 + (long long)head * c.page_size);
       }
     }
@@ -280,22 +282,23 @@ __global__ void __launch_bounds__(256, I8 ? 5 : 4) k_kv_read(KvCache c, int toke
       if (s >= steps || r >= rows) break;
       uint16_t* const dst = (r < c.heads ? K_out : V_out) + out0 + head * c.dim;
       const float inv = I8 ? __frcp_rn(gamma[s]) : 0.f;
+      const F2 by = f2(inv), g2 = f2(-gamma[s]), bias = f2(-8388736.f);
 #pragma unroll
       for (int i = 0; i < kMost; ++i) {
         if (lane + i * G >= pieces) continue;
         if constexpr (!I8) {
-          *reinterpret_cast<decltype(raw[s][i].v)*>(dst + i * G * VEC) = raw[s][i].v;
+          raw[s][i].store(dst + i * G * VEC);
         } else {
-          uint32_t word[VEC / 4];
-          if constexpr (VEC == 8) { word[0] = raw[s][i].v.x; word[1] = raw[s][i].v.y; } else word[0] = raw[s][i].v;
-          float v[VEC];
+          Bf<VEC> out;
 #pragma unroll
-          for (int k = 0; k < VEC; ++k) {
+          for (int k = 0; k < VEC / 2; ++k) {
             // under the bits of 2^23 an integer below it is itself: conversions by permute and addition
-            const float x = __uint_as_float(__byte_perm(word[k / 4] ^ 0x80808080u, 0x4B000000u, 0x7440 + k % 4)) - 8388736.f, q = __fmul_rn(x, inv);
-            v[k] = __fmaf_rn(__fmaf_rn(-q, gamma[s], x), inv, q);
+            const uint32_t word = raw[s][i].w[k / 2] ^ 0x80808080u;
+            const F2 x = f2(__uint_as_float(__byte_perm(word, 0x4B000000u, 0x7440 + 2 * (k % 2))), __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7441 + 2 * (k % 2)))) + bias;
+            const F2 q = x * by;
+            out.w[k] = pack_pair(fma2(fma2(q, g2, x), by, q));
           }
-          store_bf16<VEC>(dst + i * G * VEC, v);
+          out.store(dst + i * G * VEC);
         }
       }
     }
@@ -347,7 +350,7 @@ cudaError_t launch_kv_read(const KvCache& c, int tokens, const int* seq, const i
   auto kern = c.format == PQ_KV_INT8 ? read_kernel<true>(wide, g) : read_kernel<false>(wide, g);
   const int steps = steps_for(tokens, 2 * c.heads, g);
   LaunchScope ls(KID_KV_READ, st);
-  return launch_pdl(kern, blocks_for(tokens, 2 * c.heads, g, steps, c.format == PQ_KV_INT8 ? 5 : 4), 256, 0, st, c, tokens, seq, pos, K_out, V_out, steps);
+  return launch_pdl(kern, blocks_for(tokens, 2 * c.heads, g, steps, 4), 256, 0, st, c, tokens, seq, pos, K_out, V_out, steps);
 }
 
 }  // namespace pq

@@ -8,26 +8,11 @@
 #include <algorithm>
 #include <mutex>
 
-#include "pq_kernels.cuh"
+#include "pq_pairs.cuh"
 
 namespace pq {
 
 constexpr int kNormSmemLimit = 224 * 1024;
-
-// Pairs of fp32 numbers: one instruction multiplies and adds two of them (a third of the instructions of these kernels, which at a bf16 value
-// a tensor and element are close to being bound by them)
-struct F2 { uint64_t v; };
-__device__ __forceinline__ F2 f2(float lo, float hi) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi)); return r; }
-__device__ __forceinline__ F2 f2(float x) { return f2(x, x); }
-__device__ __forceinline__ void get(const F2& a, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a.v)); }
-__device__ __forceinline__ F2 operator*(const F2& a, const F2& b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
-__device__ __forceinline__ F2 operator+(const F2& a, const F2& b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
-__device__ __forceinline__ F2 fma2(const F2& a, const F2& b, const F2& c) {
-  F2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-  return r;
-}
-__device__ __forceinline__ float both(const F2& a) { float x, y; get(a, x, y); return x + y; }
 
 __device__ __forceinline__ void unpack8(const uint4& u, F2 (&v)[4]) {
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
