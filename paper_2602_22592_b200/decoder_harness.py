@@ -2,11 +2,16 @@
 "whole training step" workload (24 layers, hidden 2048, 16 heads, FFN 5632, RMSNorm, RoPE, vocabulary 32000 at
 full size).
 
-Only the projections are the product: each one is `pq_pack_weights` + `pq_linear_forward` in the forward pass and
+Training (`PQDecoder.step`): each projection is `pq_pack_weights` + `pq_linear_forward` in the forward pass and
 `pq_linear_backward` in the backward pass, reached through a torch.autograd.Function that marshals pointers and
-nothing else.  Everything between the projections -- embedding, RMSNorm, rotary embedding, attention, SiLU gating,
-LM head, cross-entropy -- is ordinary torch and lies outside the library's boundary; it is here so that the
-projections run in the order, on the activations and beside the foreign kernels a real QAT step gives them.
+nothing else.  Embedding, rotary embedding, attention, SiLU gating, LM head and cross-entropy are ordinary torch; so are the norms and
+the residual additions unless the model is made with `library_norms=True`: then `pq_block_norm_forward` /
+`pq_block_norm_backward` add a block's output to the stream and norm it for the next one in one pass each way.
+
+Serving (`PQServer`): prompts and then one token per sequence at a time.  Projections run from the packed sign bits
+(`pq_decode_batch`) or, for prompts, on the tensor cores; keys and values live in a paged cache (`pq_kv_append`, bf16 or int8), a new
+token attends over it with `pq_attn_decode`, a prompt over its history as `pq_kv_read` gives it back, and
+`pq_block_norm_forward` stands between the blocks.  SiLU gating, the prompt's attention and the LM head are torch.
 
 CUDA events around every pq_* call let the caller report the pQuant-linear time of a step apart from the rest.
 """
@@ -18,6 +23,8 @@ import torch
 import torch.nn.functional as F
 
 from . import binding as pqb
+
+NORM_EPS = 1e-5
 
 
 class _Workspaces:
@@ -140,6 +147,40 @@ class PQLinearModule:
         return dx
 
 
+class _NormFn(torch.autograd.Function):
+    """(x, y, weight) -> x + y and its RMSNorm times weight; without y the norm of x alone (the first one of a model)."""
+
+    @staticmethod
+    def forward(ctx, x, y, weight, mod):
+        ctx.set_materialize_grads(False)
+        x = x.contiguous()
+        h = torch.empty_like(x)
+        out = x if y is None else torch.empty_like(x)
+        y = None if y is None else y.contiguous()
+        pqb.pq_block_norm_forward(mod.norm_desc, x, y, None, None, weight.detach(), None if y is None else out, h)
+        ctx.mod, ctx.joined = mod, y is not None
+        ctx.save_for_backward(out, weight)
+        if mod.norm_capture is not None:
+            mod.norm_capture.append(dict(x=x.detach().clone(), y=None if y is None else y.detach().clone(), weight=weight.detach().clone(), h=h.clone(),
+                                         x_out=out.detach().clone()))
+            ctx.capture = mod.norm_capture[-1]
+        return (out, h) if ctx.joined else h
+
+    @staticmethod
+    def backward(ctx, *grads):
+        out, weight = ctx.saved_tensors
+        dx_out, dh = grads if ctx.joined else (None, grads[0])
+        dx_out, dh = (None if g is None else g.contiguous() for g in (dx_out, dh))
+        if dh is None:                        # nothing came back through the norm
+            return dx_out, dx_out if ctx.joined else None, None, None
+        dx = torch.empty_like(out)
+        dweight = torch.empty(weight.numel(), dtype=torch.float32, device=out.device)
+        pqb.pq_block_norm_backward(ctx.mod.norm_desc, dx_out, dh, out, None, None, None, weight.detach(), dx, None, None, None, dweight, ctx.mod.norm_ws)
+        if ctx.mod.norm_capture is not None:
+            ctx.capture.update(dx_out=None if dx_out is None else dx_out.clone(), dh=dh.clone(), dx=dx.clone(), dweight=dweight.clone())
+        return dx, dx if ctx.joined else None, dweight.to(weight.dtype), None
+
+
 def _rope_tables(seq, head_dim, device, base=10000.0):
     inv = 1.0 / (base ** (torch.arange(0, head_dim, 2, device=device, dtype=torch.float32) / head_dim))
     ang = torch.outer(torch.arange(seq, device=device, dtype=torch.float32), inv)     # [S, D/2]
@@ -158,7 +199,7 @@ class PQDecoder:
     paper gives its attention blocks (Sec. 3); True gives them the same routed HP branch as the MLP projections."""
 
     def __init__(self, layers=24, hidden=2048, heads=16, ffn=5632, vocab=32000, batch=4, seq=2048, r=128, E=8, attn_hp=True,
-                 device="cuda:0", seed=3):
+                 device="cuda:0", seed=3, library_norms=False):
         self.dev = torch.device(device)
         self.layers, self.hidden, self.heads, self.ffn, self.vocab, self.batch, self.seq = layers, hidden, heads, ffn, vocab, batch, seq
         self.head_dim = hidden // heads
@@ -183,6 +224,11 @@ class PQDecoder:
         self.norm_f = torch.ones(hidden, device=self.dev, dtype=torch.bfloat16, requires_grad=True)
         self.cos, self.sin = _rope_tables(seq, self.head_dim, self.dev)
         self.gen = gen
+        self.library_norms = library_norms
+        self.norm_capture = None      # set to a list by tests: receives a dict for every norm of the next step
+        if library_norms:
+            self.norm_desc = pqb.make_norm_desc(T, hidden, NORM_EPS)
+            self.norm_ws = torch.empty(pqb.pq_block_norm_workspace_bytes(self.norm_desc), dtype=torch.uint8, device=self.dev)
 
     def linears(self):
         for blk in self.blocks:
@@ -205,21 +251,29 @@ class PQDecoder:
         for p in self._torch_params():
             p.grad = None
         B, S, H, D = self.batch, self.seq, self.heads, self.head_dim
+        lib = self.library_norms
+        norm = lambda x, w: _NormFn.apply(x, None, w, self) if lib else F.rms_norm(x, (self.hidden,), w, NORM_EPS)
+
+        def join(x, y, w):
+            """The stream behind a block, and the next block's input."""
+            if lib:
+                return _NormFn.apply(x, y, w, self)
+            x = x + y
+            return x, F.rms_norm(x, (self.hidden,), w, NORM_EPS)
+
         x = F.embedding(ids, self.embed).view(B * S, self.hidden)
-        for blk in self.blocks:
-            h = F.rms_norm(x, (self.hidden,), blk["norm1"], 1e-5)
+        h = norm(x, self.blocks[0]["norm1"])
+        for i, blk in enumerate(self.blocks):
             q = blk["q"](h).view(B, S, H, D).transpose(1, 2)
             k = blk["k"](h).view(B, S, H, D).transpose(1, 2)
             v = blk["v"](h).view(B, S, H, D).transpose(1, 2)
             q, k = _apply_rope(q, self.cos, self.sin), _apply_rope(k, self.cos, self.sin)
             a = F.scaled_dot_product_attention(q, k, v, is_causal=True)
             a = a.transpose(1, 2).reshape(B * S, self.hidden)
-            x = x + blk["o"](a)
-            h = F.rms_norm(x, (self.hidden,), blk["norm2"], 1e-5)
+            x, h = join(x, blk["o"](a), blk["norm2"])
             m = F.silu(blk["gate"](h)) * blk["up"](h)
-            x = x + blk["down"](m)
-        x = F.rms_norm(x, (self.hidden,), self.norm_f, 1e-5)
-        logits = x @ self.head.t()
+            x, h = join(x, blk["down"](m), self.blocks[i + 1]["norm1"] if i + 1 < self.layers else self.norm_f)
+        logits = h @ self.head.t()
         loss = F.cross_entropy(logits.float(), tgt.view(-1))
         loss.backward()
         return loss.detach()
@@ -231,6 +285,142 @@ class PQDecoder:
             tnk = L.T * L.N * L.K
             t += 2 * tnk / p_i8 + (4 * tnk + 6 * L.T * L.r * (L.K + L.N)) / p_bf16
         return t
+
+
+class PQServer:
+    """Serves a PQDecoder's weights to `n` sequences (16 at most: the decode path's tokens): `prompt` takes their first tokens, or more of
+    them later, `step` one new token each; both return the logits of every sequence's last token [n, vocab].
+
+    The cache has room for `positions` tokens a sequence in pages of `page_size`, handed out as sequences grow; lengths live on the
+    host (a program that admits and frees sequences does so there) and on the device.  Weights are packed when the server is made."""
+
+    def __init__(self, model: PQDecoder, n, positions, page_size=64, int8_cache=False):
+        assert 1 <= n <= 16
+        self.m, self.n, self.positions = model, n, positions
+        dev, H, D, L = model.dev, model.heads, model.head_dim, model.layers
+        self.dev = dev
+        self.entries = -(-positions // page_size)
+        pages = n * self.entries
+        pitch = pqb.pq_kv_pitch(pqb.PQ_KV_INT8 if int8_cache else pqb.PQ_KV_BF16, D)
+        self.table = torch.full((n, self.entries), -1, dtype=torch.int32, device=dev)
+        self.free = list(range(pages - 1, -1, -1))
+        self.page_size, self.held = page_size, [0] * n
+        shape = (pages, H, page_size, pitch)
+        pages_of = lambda: torch.zeros(shape, dtype=torch.int8 if int8_cache else torch.bfloat16, device=dev)
+        gammas = lambda: torch.ones(shape[:3], device=dev) if int8_cache else None
+        self.caches = [pqb.make_kv_cache(pages_of(), pages_of(), self.table, D, gammas(), gammas()) for _ in range(L)]     # one table, a cache a layer
+        self.cos, self.sin = _rope_tables(positions, D, dev)
+        self.attn_ws = torch.empty(pqb.pq_attn_workspace_bytes(self.caches[0], H), dtype=torch.uint8, device=dev)
+        self.seq = torch.arange(n, dtype=torch.int32, device=dev)
+        self.desc = pqb.make_norm_desc(n, model.hidden, NORM_EPS)
+        self.capture = None       # set to a list by tests: receives a dict for every layer of the next call
+        for lin in model.linears():
+            pqb.pq_pack_weights(lin.desc, lin.W, lin.w_bits, lin.w_s8, lin.w_scales, model.ws.pack)
+        self.items = [{names: self._items(blk, names) for names in (("q", "k", "v"), ("o",), ("gate", "up"), ("down",))} for blk in model.blocks]
+
+    def _items(self, blk, names):
+        """Decode descriptors of linears that read the same tokens, with their inputs, outputs and workspaces."""
+        lins = [blk[k] for k in names]
+        x = torch.empty((self.n, lins[0].K), dtype=torch.bfloat16, device=self.dev)
+        ys, entries, keep = [], [], []
+        for lin in lins:
+            d = pqb.make_desc(self.n, lin.K, lin.N, lin.r, lin.E)
+            ys.append(torch.empty((self.n, lin.N), dtype=torch.bfloat16, device=self.dev))
+            nb, nB = pqb.pq_decode_pack_bytes(d)
+            bits = torch.empty(nb, dtype=torch.uint8, device=self.dev)
+            b_il = torch.empty(nB, dtype=torch.uint8, device=self.dev) if nB else None
+            pqb.pq_pack_decode(d, lin.w_bits, lin.B, bits, b_il)
+            ws = torch.zeros(max(16, pqb.pq_workspace_bytes(d, pqb.PQ_PHASE_DECODE)), dtype=torch.uint8, device=self.dev)
+            entries.append((d, x, lin.w_bits, lin.w_scales, lin.A, lin.B, lin.Wr, lin.alpha, lin.beta, ys[-1], ws, None, 0.0, bits, b_il))
+            keep += [bits, b_il, ws]
+        return x, ys, pqb.make_decode_items(entries), keep
+
+    def _grow(self, more):
+        """Pages for more[s] further tokens of sequence s; nothing changes where one of them has no room."""
+        for s, k in enumerate(more):
+            if self.held[s] + k > self.positions:
+                raise ValueError(f"sequence {s}: {self.held[s] + k} tokens, there is room for {self.positions}")
+        for s, k in enumerate(more):
+            have, need = -(-self.held[s] // self.page_size), -(-(self.held[s] + k) // self.page_size)
+            if need > have:
+                ids = [self.free.pop() for _ in range(need - have)]
+                self.table[s, have:need] = torch.tensor(ids, dtype=torch.int32, device=self.dev)
+        self.held = [h + k for h, k in zip(self.held, more)]
+
+    def _decode(self, i, names, x):
+        xin, ys, items, _ = self.items[i][names]
+        xin.copy_(x)
+        pqb.pq_decode_batch(items)
+        return ys
+
+    def step(self, ids):
+        """One new token of every sequence: ids [n]."""
+        m, n = self.m, self.n
+        self._grow([1] * n)
+        lens = torch.tensor(self.held, dtype=torch.int32, device=self.dev)
+        pos = lens - 1
+        x = m.embed.detach()[ids]
+        h, q_rot, a = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+        pqb.pq_block_norm_forward(self.desc, x, None, None, None, m.blocks[0]["norm1"].detach(), None, h)
+        for i, blk in enumerate(m.blocks):
+            q, k, v = self._decode(i, ("q", "k", "v"), h)
+            pqb.pq_kv_append(self.caches[i], self.seq, pos, k, v, self.cos, self.sin, q, q_rot)
+            pqb.pq_attn_decode(self.caches[i], q_rot, lens, m.head_dim ** -0.5, a, None, self.attn_ws)
+            if self.capture is not None:
+                self.capture.append(dict(q=q.clone(), k=k.clone(), v=v.clone(), q_rot=q_rot.clone(), a=a.clone(), lens=lens.clone(), x=x.clone()))
+            y, = self._decode(i, ("o",), a)
+            pqb.pq_block_norm_forward(self.desc, x, y, None, None, blk["norm2"].detach(), x, h)
+            if self.capture is not None:
+                self.capture[-1].update(o=y.clone(), x_out=x.clone(), h=h.clone())
+            gate, up = self._decode(i, ("gate", "up"), h)
+            y, = self._decode(i, ("down",), F.silu(gate) * up)
+            pqb.pq_block_norm_forward(self.desc, x, y, None, None, (m.blocks[i + 1]["norm1"] if i + 1 < m.layers else m.norm_f).detach(), x, h)
+        return h @ m.head.detach().t()
+
+    def prompt(self, ids, lengths):
+        """lengths[s] further tokens of every sequence (host integers, at least 1), ids [n, max(lengths)]; what lies behind a sequence's own
+        tokens is padding.  They attend over what the sequence holds already, and over one another in order."""
+        m, n, S = self.m, self.n, ids.shape[1]
+        assert len(lengths) == n and max(lengths) == S and min(lengths) >= 1
+        past = list(self.held)
+        self._grow(lengths)
+        T, H, D, dev = n * S, m.heads, m.head_dim, self.dev
+        at = torch.arange(S, device=dev)[None]
+        begin, count = torch.tensor(past, device=dev)[:, None], torch.tensor(lengths, device=dev)[:, None]
+        pos = torch.where(at < count, begin + at, -1).to(torch.int32).reshape(-1)
+        seq = torch.arange(n, dtype=torch.int32, device=dev).repeat_interleave(S)
+        most = max(self.held)
+        all_at = torch.arange(most, device=dev)[None]
+        held = torch.tensor(self.held, device=dev)[:, None]
+        all_pos = torch.where(all_at < held, all_at, -1).to(torch.int32).reshape(-1)
+        all_seq = torch.arange(n, dtype=torch.int32, device=dev).repeat_interleave(most)
+        mask = all_at[:, None, :] <= (begin + at)[:, :, None]                                  # [n, S, most]
+        desc = pqb.make_norm_desc(T, m.hidden, NORM_EPS)
+        x = m.embed.detach()[ids].reshape(T, m.hidden)
+        h, q_rot = torch.empty_like(x), torch.empty_like(x)
+        pqb.pq_block_norm_forward(desc, x, None, None, None, m.blocks[0]["norm1"].detach(), None, h)
+
+        def linear(lin, x):
+            d = pqb.make_desc(T, lin.K, lin.N, lin.r, lin.E)
+            y = torch.empty((T, lin.N), dtype=torch.bfloat16, device=dev)
+            ws = torch.empty(pqb.pq_workspace_bytes(d, pqb.PQ_PHASE_FWD), dtype=torch.uint8, device=dev)
+            pqb.pq_linear_forward(d, x, lin.w_bits, lin.w_s8, lin.w_scales, lin.A, lin.B, lin.Wr, lin.alpha, lin.beta, y, None, ws)
+            return y
+
+        for i, blk in enumerate(m.blocks):
+            q, k, v = (linear(blk[name], h) for name in "qkv")
+            q_rot.zero_()                                       # rows of padding are left as they are
+            pqb.pq_kv_append(self.caches[i], seq, pos, k, v, self.cos, self.sin, q, q_rot)
+            ks, vs = (torch.zeros((n * most, H * D), dtype=torch.bfloat16, device=dev) for _ in range(2))
+            pqb.pq_kv_read(self.caches[i], all_seq, all_pos, ks, vs)
+            heads = lambda t, rows: t.view(n, rows, H, D).transpose(1, 2)
+            a = F.scaled_dot_product_attention(heads(q_rot, S), heads(ks, most), heads(vs, most), attn_mask=mask[:, None])
+            y = linear(blk["o"], a.transpose(1, 2).reshape(T, m.hidden))
+            pqb.pq_block_norm_forward(desc, x, y, None, None, blk["norm2"].detach(), x, h)
+            y = linear(blk["down"], F.silu(linear(blk["gate"], h)) * linear(blk["up"], h))
+            pqb.pq_block_norm_forward(desc, x, y, None, None, (m.blocks[i + 1]["norm1"] if i + 1 < m.layers else m.norm_f).detach(), x, h)
+        last = torch.arange(n, device=dev) * S + count[:, 0] - 1
+        return h[last] @ m.head.detach().t()
 
 
 def softmax_entropy_bound(vocab):

@@ -620,3 +620,123 @@ def test_norm_gradients_against_differences_of_the_kernel():
     noise = 6 * np.sqrt(2 * 2 * T * N) * 2 * HALF / np.sqrt(3) / (2 * step)
     # x_out's rounding reaches g through the backward as well (2^-8 of g), and the cubic term of the difference: 0.05^2
     assert abs(slope - (g * g).sum()) <= noise + (HALF + 0.01) * (g * g).sum()
+
+
+# --------------------------------------------------------------------------- together, as a decoder uses them
+from paper_2602_22592_b200.decoder_harness import NORM_EPS, PQDecoder, PQServer  # noqa: E402
+
+
+def bf16_sum_tol(x, y):
+    return HALF * np.abs(x + y) + 2.0 ** -23 * (np.abs(x) + np.abs(y)) + 1e-38
+
+
+def close_norm(h, s, w, tol_s):
+    """h against the norm of s (64 bits), s known to tol_s."""
+    want = B.rms(s, NORM_EPS) * w
+    r = 1 / np.sqrt((s * s).mean(-1, keepdims=True) + NORM_EPS)
+    whole = np.sqrt((tol_s * tol_s).sum(-1, keepdims=True) / ((s * s).sum(-1, keepdims=True) + 1e-30))
+    tol = HALF * np.abs(want) + (s.shape[-1] + 16) * 2.0 ** -24 * np.abs(want) + np.abs(tol_s * r * w) + np.abs(want) * whole + 1e-38
+    assert (np.abs(h - want) <= tol).all()
+
+
+@pytest.mark.parametrize("int8,heads,page", [(False, 4, 16), (True, 4, 32), (True, 2, 16)])
+def test_server_prompts_and_steps(int8, heads, page):
+    # prompts of different lengths, steps, a further ragged prompt, steps across page ends; every attention and norm of the steps against the
+    # 64-bit forms on what the cache holds
+    m = PQDecoder(layers=2, hidden=256, heads=heads, ffn=512, vocab=500, batch=1, seq=64, r=32, E=4, seed=7)
+    n, D = 3, 256 // heads
+    S = PQServer(m, n, 70, page, int8)
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(1)
+    ids = lambda *shape: torch.randint(0, 500, shape, generator=gen, device=DEV)  # noqa: E731
+    logits = S.prompt(ids(n, 29), [29, 1, 13])
+    assert logits.shape == (n, 500) and torch.isfinite(logits.float()).all()
+
+    def steps(k):
+        for _ in range(k):
+            S.capture = []
+            out = S.step(ids(n))
+            torch.cuda.synchronize()
+            check_status()
+            assert torch.isfinite(out.float()).all() and len(S.capture) == 2
+            for i, cap in enumerate(S.capture):
+                lens = [int(v) for v in cap["lens"]]
+                assert lens == S.held
+                cos, sin = S.cos[[v - 1 for v in lens]].cpu().numpy(), S.sin[[v - 1 for v in lens]].cpu().numpy()
+                q = B.rope(f64(cap["q"]).reshape(n, heads, D), cos, sin)
+                assert np.array_equal(f64(cap["q_rot"]).reshape(q.shape), q)
+                k_new = B.rope(f64(cap["k"]).reshape(n, heads, D), cos, sin)
+                rows = []
+                for s in range(n):
+                    seq = torch.full((lens[s],), s, dtype=torch.int32, device=DEV)
+                    pos = torch.arange(lens[s], dtype=torch.int32, device=DEV)
+                    ko, vo = (torch.empty((lens[s], heads * D), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+                    pqb.pq_kv_read(S.caches[i], seq, pos, ko, vo)
+                    pair = []
+                    table = S.table.cpu().numpy()
+                    p = np.arange(lens[s])
+                    for pages, gam in ((S.caches[i].tensors[0], S.caches[i].tensors[3]), (S.caches[i].tensors[1], S.caches[i].tensors[4])):
+                        x = pages.float().cpu().numpy().astype(np.float64)[table[s, p // page], :, p % page, :D]
+                        if int8:
+                            x = x / gam.cpu().numpy().astype(np.float64)[table[s, p // page], :, p % page][..., None]
+                        pair.append(x)
+                    assert np.array_equal(f64(ko).reshape(pair[0].shape), B.bf16(pair[0].astype(np.float32)) if int8 else pair[0])
+                    last = k_new[s] if not int8 else (lambda c, g: c / g.astype(np.float64)[:, None])(*B.quantise(k_new[s]))
+                    assert np.array_equal(pair[0][-1], last)
+                    rows.append(pair)
+                close_attention(cap["a"], None, q, rows, D ** -0.5, int8)
+                x, o = f64(cap["x"]), f64(cap["o"])
+                tol = bf16_sum_tol(x, o)
+                assert (np.abs(f64(cap["x_out"]) - (x + o)) <= tol).all()
+                close_norm(f64(cap["h"]), x + o, f64(m.blocks[i]["norm2"]), 2.0 ** -23 * (np.abs(x) + np.abs(o)))
+            S.capture = None
+
+    steps(4)
+    S.prompt(ids(n, 9), [1, 9, 4])
+    assert S.held == [34, 14, 21]
+    steps(2)
+    with pytest.raises(ValueError):
+        S.prompt(ids(n, 60), [60, 60, 60])
+
+
+def test_server_refuses_nothing_it_has_room_for():
+    m = PQDecoder(layers=1, hidden=128, heads=2, ffn=256, vocab=100, batch=1, seq=32, r=0, E=0, seed=8)
+    S = PQServer(m, 2, 33, 16)
+    S.prompt(torch.zeros((2, 33), dtype=torch.int64, device=DEV), [33, 20])
+    assert S.held == [33, 20] and len({int(v) for v in S.table.flatten() if v >= 0}) == 5
+    torch.cuda.synchronize()
+    check_status()
+
+
+def test_training_step_with_library_norms():
+    # every norm of a step, forward and backward, against the 64-bit forms on its own inputs
+    m = PQDecoder(layers=2, hidden=256, heads=4, ffn=512, vocab=400, batch=2, seq=32, r=32, E=4, seed=9, library_norms=True)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(2)
+    with torch.no_grad():
+        for p in [m.norm_f] + [b[k] for b in m.blocks for k in ("norm1", "norm2")]:
+            p.copy_(1 + 0.2 * torch.randn(256, generator=g, device=DEV))
+    ids, tgt = m.random_batch()
+    m.norm_capture = []
+    loss = m.step(ids, tgt)
+    torch.cuda.synchronize()
+    check_status()
+    assert torch.isfinite(loss) and len(m.norm_capture) == 5
+    weights = [m.blocks[0]["norm1"], m.blocks[0]["norm2"], m.blocks[1]["norm1"], m.blocks[1]["norm2"], m.norm_f]
+    for cap, weight in zip(m.norm_capture, weights):
+        x, w = f64(cap["x"]), f64(cap["weight"])
+        y = None if cap["y"] is None else f64(cap["y"])
+        s = x if y is None else x + y
+        if y is not None:
+            assert (np.abs(f64(cap["x_out"]) - s) <= bf16_sum_tol(x, y)).all()
+        close_norm(f64(cap["h"]), s, w, np.zeros_like(s) if y is None else 2.0 ** -23 * (np.abs(x) + np.abs(y)))
+        ds = None if cap.get("dx_out") is None else f64(cap["dx_out"])
+        dh, st = f64(cap["dh"]), f64(cap["x_out"])
+        want = B.block_norm_backward(ds, dh, st, None, None, None, w, 1.0, NORM_EPS)
+        r = 1 / np.sqrt((st * st).mean(-1, keepdims=True) + NORM_EPS)
+        size = (0 if ds is None else np.abs(ds)) + r * (np.abs(dh * w) + np.abs(st * r) * np.abs(dh * w * st * r).mean(-1, keepdims=True))
+        assert (np.abs(f64(cap["dx"]) - want["dx"]) <= HALF * np.abs(want["dx"]) + (256 + 24) * 2.0 ** -24 * size + 1e-38).all()
+        tol = (len(st) + 256 + 32) * 2.0 ** -24 * np.abs(dh * st * r).sum(0)
+        assert (np.abs(f64(cap["dweight"]) - want["dpre"]) <= tol + 1e-38).all()
+        assert torch.equal(weight.grad, cap["dweight"].to(torch.bfloat16))
+    assert (m.norm_capture[-1]["dx_out"] if "dx_out" in m.norm_capture[-1] else None) is None      # nothing reads the stream behind the last norm
