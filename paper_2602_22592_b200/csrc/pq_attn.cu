@@ -424,7 +424,7 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
 #pragma unroll
     for (int s = 0; s < F::kStages - 1; ++s) issue(s);
     // counts of the items that this CTA may share: the one that it begins inside of, and one that begins here (while the first loads are on their way)
-    if (lane == 0 && (r0 == c0 || r1 == c1)) {
+    if (lane == 0 && (r0 == c0 || r1 == c1) && !(sh.by_chunk && cta_share[3] == 1)) {
       if (r0 == c0 && cw.t0 > 0) {
         const long long x0 = r0 - cw.t0;
         open[0].first = sh.by_chunk ? (int)cta_share[2] : sh.holder(x0);

@@ -176,7 +176,6 @@ __global__ void __launch_bounds__(256, VEC == 8 ? 2 : 3) k_kv_append(KvCache c, 
       for (int i = 0; i < kMost; ++i) {
         if (lane + i * G >= pieces) continue;
         if (turns && key) {
-          // products and sums one by one (of pairs they came out fused, one rounding short)
 #pragma unroll
           for (int k = 0; k < VEC / 2; ++k) {
             float c0, c1, s0, s1;

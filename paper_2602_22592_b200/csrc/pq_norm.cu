@@ -47,49 +47,52 @@ __device__ __forceinline__ void norm_copy_wait(int pending) {
 
 // Rows of up to four tensors on their way through shared memory by asynchronous copies, [stage][tensor][piece][thread]: a thread copies what it
 // will read itself, so that nothing has to be waited for but its own copies.  Pieces behind the row's end and absent tensors
-// stay zero.
-template <int K, int CH, int RB>
+// stay zero.  THREADS, the most a block can have, is the stride, so that every place is an offset the compiler knows: with strides and
+// rows multiplied out at every access half of these kernels' instructions were integer ones.
+template <int K, int CH, int RB, int THREADS>
 struct RowRing {
-  uint4* base;               // this thread's column of its team's part
-  const uint16_t* from[K];
-  long long ahead, step;
-  int lanes, l, chunks, N, T, stages, stage, into;      // stages: as many rows as are worked on at once (RB), and those on their way
-  __device__ uint4* place(int s, int k, int i) const { return base + (size_t)((s * K + k) * CH + i) * lanes; }
+  static constexpr int kPiece = THREADS * 16, kStage = K * CH * kPiece;
+  uint8_t* base;             // this thread's column
+  const uint16_t* from[K];   // this thread's first piece of the next row to ask for, or null
+  long long left, hop;       // rows of this team still to ask for; values from one to the next
+  int gap, mine;             // values from piece to piece of a thread; how many pieces it has
+  int most, at, into;        // bytes of the stages; where the row at work, the next copies are
   __device__ void begin() {
-    for (int s = 0; s < stages; ++s)
+    for (int s = 0; s < most; s += kStage)
 #pragma unroll
       for (int k = 0; k < K; ++k)
 #pragma unroll
         for (int i = 0; i < CH; ++i)
-          if (!from[k] || l + i * lanes >= chunks) *place(s, k, i) = make_uint4(0, 0, 0, 0);
-    stage = 0;
-    into = stages - RB;
-    for (int s = 0; s < stages - RB; ++s) issue(s);
+          if (!from[k] || i >= mine) *reinterpret_cast<uint4*>(base + s + (k * CH + i) * kPiece) = make_uint4(0, 0, 0, 0);
+    at = into = 0;
+    for (int s = 0; s < most / kStage - RB; ++s) issue();
   }
-  __device__ void issue(int s) {
-    if (ahead < T) {
+  __device__ void issue() {
+    if (left > 0) {
+      const uint32_t dst = smem_u32(base) + into;
 #pragma unroll
-      for (int k = 0; k < K; ++k)
+      for (int k = 0; k < K; ++k) {
+        if (!from[k]) continue;
 #pragma unroll
         for (int i = 0; i < CH; ++i)
-          if (from[k] && l + i * lanes < chunks) cp_async16(smem_u32(place(s, k, i)), from[k] + ahead * N + (l + i * lanes) * 8, true);
+          if (i < mine) cp_async16(dst + (k * CH + i) * kPiece, from[k] + i * gap, true);
+        from[k] += hop;
+      }
+      --left;
     }
-    ahead += step;
+    into = into + kStage == most ? 0 : into + kStage;
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
-  __device__ int after(int s) const { return s + 1 == stages ? 0 : s + 1; }
+  __device__ int after(int s) const { return s + kStage == most ? 0 : s + kStage; }
   __device__ void next() {                                     // the RB rows to work on are there, those behind them on their way
 #pragma unroll
-    for (int b = 0; b < RB; ++b) {
-      issue(into);
-      into = after(into);
-    }
-    norm_copy_wait(stages - RB);
+    for (int b = 0; b < RB; ++b) issue();
+    norm_copy_wait(most / kStage - RB);
   }
-  __device__ uint4 get(int b, int k, int i) const { return *place(b == 0 ? stage : after(stage), k, i); }
+  __device__ uint4 get(int b, int k, int i) const { return *reinterpret_cast<const uint4*>(base + (b == 0 ? at : after(at)) + (k * CH + i) * kPiece); }
   __device__ void done() {
 #pragma unroll
-    for (int b = 0; b < RB; ++b) stage = after(stage);
+    for (int b = 0; b < RB; ++b) at = after(at);
   }
 };
 
@@ -128,8 +131,9 @@ __host__ __device__ constexpr int team_floats(int warps) { return 2 * 8 * warps;
 // k_block_norm: `warps` warps per row, CH pieces of 8 values per thread; teams of warps walk the rows with a stride.  The gains of a
 // thread's columns stay in its registers.
 // ---------------------------------------------------------------------------
+template <int CH> constexpr int kNormThreads = CH == 1 ? 1024 : 512;
 template <int CH, bool Y, bool POST>
-__global__ void __launch_bounds__(CH == 1 ? 1024 : 512) k_block_norm(const __grid_constant__ BlockNormArgs a, int warps, int stages) {
+__global__ void __launch_bounds__(kNormThreads<CH>) k_block_norm(const __grid_constant__ BlockNormArgs a, int warps, int stages) {
   extern __shared__ float smem_f[];
   pdl_launch_dependents();
   constexpr int K = Y ? 2 : 1;
@@ -138,12 +142,15 @@ __global__ void __launch_bounds__(CH == 1 ? 1024 : 512) k_block_norm(const __gri
   const int chunks = a.N / 8;
   long long row = (long long)blockIdx.x * teams + team;
   const long long step = (long long)gridDim.x * teams;
-  RowRing<K, CH, 1> ring;
-  ring.base = reinterpret_cast<uint4*>(smem_f + teams * team_floats(warps)) + (size_t)team * stages * K * CH * lanes + l;
-  ring.from[0] = a.x;
-  if (Y) ring.from[K - 1] = a.y;
-  ring.ahead = row; ring.step = step;
-  ring.lanes = lanes; ring.l = l; ring.chunks = chunks; ring.N = a.N; ring.T = a.T; ring.stages = stages;
+  const int mine = l < chunks ? min(CH, (chunks - l + lanes - 1) / lanes) : 0, gap = lanes * 8;
+  long long off = row * a.N + l * 8;                           // of this thread's first piece of the row
+  const long long hop = step * a.N;
+  RowRing<K, CH, 1, kNormThreads<CH>> ring;
+  ring.base = reinterpret_cast<uint8_t*>(smem_f + teams * team_floats(warps)) + tid * 16;
+  ring.from[0] = a.x + off;
+  if (Y) ring.from[K - 1] = a.y + off;
+  ring.left = row < a.T ? (a.T - row + step - 1) / step : 0;
+  ring.hop = hop; ring.gap = gap; ring.mine = mine; ring.most = stages * ring.kStage;
   pdl_wait();
   ring.begin();
   const float gate1 = a.gate && !a.gate_vector ? __ldcg(a.gate) : 1.f, inv_n = 1.f / a.N;
@@ -151,10 +158,10 @@ __global__ void __launch_bounds__(CH == 1 ? 1024 : 512) k_block_norm(const __gri
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
     const int c = l + i * lanes;
-    pre[i] = a.h && c < chunks ? ldcg8(a.pre, c) : make_uint4(0, 0, 0, 0);
-    if (POST) post[POST ? i : 0] = c < chunks ? ldcg8(a.post, c) : make_uint4(0, 0, 0, 0);
+    pre[i] = a.h && i < mine ? ldcg8(a.pre, c) : make_uint4(0, 0, 0, 0);
+    if (POST) post[POST ? i : 0] = i < mine ? ldcg8(a.post, c) : make_uint4(0, 0, 0, 0);
   }
-  for (; row < a.T; row += step) {
+  for (; row < a.T; row += step, off += hop) {
     ring.next();
     float ry = 1.f;
     if (POST) {
@@ -174,7 +181,6 @@ __global__ void __launch_bounds__(CH == 1 ? 1024 : 512) k_block_norm(const __gri
     F2 s[CH][4], sq = f2(0.f);
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      const int c = l + i * lanes;
       unpack8(ring.get(0, 0, i), s[i]);
       F2 u[4];
       if (Y) {
@@ -187,8 +193,9 @@ __global__ void __launch_bounds__(CH == 1 ? 1024 : 512) k_block_norm(const __gri
 #pragma unroll
           for (int k = 0; k < 4; ++k) u[k] = u[k] * w[k];
         }
-        if (a.gate_vector && c < chunks) {                     // 32 bytes a piece: read again, from L1
-          const float4 g0 = __ldca(reinterpret_cast<const float4*>(a.gate) + 2 * c), g1 = __ldca(reinterpret_cast<const float4*>(a.gate) + 2 * c + 1);
+        if (a.gate_vector && i < mine) {                       // 32 bytes a piece: read again, from L1
+          const float4* at = reinterpret_cast<const float4*>(a.gate + l * 8 + i * gap);
+          const float4 g0 = __ldca(at), g1 = __ldca(at + 1);
           u[0] = u[0] * f2(g0.x, g0.y); u[1] = u[1] * f2(g0.z, g0.w); u[2] = u[2] * f2(g1.x, g1.y); u[3] = u[3] * f2(g1.z, g1.w);
         }
       }
@@ -197,7 +204,7 @@ __global__ void __launch_bounds__(CH == 1 ? 1024 : 512) k_block_norm(const __gri
         s[i][k] = Y ? fma2(scale, s[i][k], u[k]) : scale * s[i][k];
         sq = fma2(s[i][k], s[i][k], sq);
       }
-      if (a.x_out && c < chunks) reinterpret_cast<uint4*>(a.x_out + row * a.N)[c] = pack8(s[i]);
+      if (a.x_out && i < mine) *reinterpret_cast<uint4*>(a.x_out + off + i * gap) = pack8(s[i]);
     }
     ring.done();
     if (!a.h) continue;
@@ -206,13 +213,12 @@ __global__ void __launch_bounds__(CH == 1 ? 1024 : 512) k_block_norm(const __gri
     const F2 r = f2(rsqrtf(v[0] * inv_n + a.eps));
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-      const int c = l + i * lanes;
-      if (c >= chunks) continue;
+      if (i >= mine) continue;
       F2 w[4];
       unpack8(pre[i], w);
 #pragma unroll
       for (int k = 0; k < 4; ++k) w[k] = s[i][k] * r * w[k];
-      reinterpret_cast<uint4*>(a.h + row * a.N)[c] = pack8(w);
+      *reinterpret_cast<uint4*>(a.h + off + i * gap) = pack8(w);
     }
   }
   norm_copy_wait<0>();
@@ -239,14 +245,17 @@ __global__ void __launch_bounds__(512, 1) k_block_norm_backward(const __grid_con
   const long long step = (long long)gridDim.x * teams;
   long long row = (long long)blockIdx.x * teams + team;
   constexpr int RB = CH == 4 ? 1 : 2;                          // rows worked on at once: their sums meet in the same barriers
-  RowRing<K, CH, RB> ring;
-  ring.base = reinterpret_cast<uint4*>(smem_f + teams * team_floats(warps)) + (size_t)team * stages * K * CH * lanes + l;
-  ring.from[0] = a.dh ? a.x : nullptr;
-  ring.from[1] = a.dh;
-  ring.from[2] = a.dx_out;
-  if (kY) ring.from[K - 1] = a.y;
-  ring.ahead = row; ring.step = step;
-  ring.lanes = lanes; ring.l = l; ring.chunks = chunks; ring.N = a.N; ring.T = a.T; ring.stages = stages;
+  const int mine = l < chunks ? min(CH, (chunks - l + lanes - 1) / lanes) : 0, gap = lanes * 8;
+  long long off = row * a.N + l * 8;                           // of this thread's first piece of the row
+  const long long hop = step * a.N;
+  RowRing<K, CH, RB, 512> ring;
+  ring.base = reinterpret_cast<uint8_t*>(smem_f + teams * team_floats(warps)) + tid * 16;
+  ring.from[0] = a.dh ? a.x + off : nullptr;
+  ring.from[1] = a.dh ? a.dh + off : nullptr;
+  ring.from[2] = a.dx_out ? a.dx_out + off : nullptr;
+  if (kY) ring.from[K - 1] = a.y + off;
+  ring.left = row < a.T ? (a.T - row + step - 1) / step : 0;
+  ring.hop = hop; ring.gap = gap; ring.mine = mine; ring.most = stages * ring.kStage;
   pdl_wait();
   ring.begin();
   const float gate1 = GATE == 1 ? __ldcg(a.gate) : 1.f, inv_n = 1.f / a.N;
@@ -259,7 +268,7 @@ __global__ void __launch_bounds__(512, 1) k_block_norm_backward(const __grid_con
 #pragma unroll
   for (int i = 0; i < CH; ++i) {
     const int c = l + i * lanes;
-    const bool ok = c < chunks;
+    const bool ok = i < mine;
     pre[i] = ok && a.dh ? ldcg8(a.pre, c) : make_uint4(0, 0, 0, 0);
     if (POST) post[POST ? i : 0] = ok ? ldcg8(a.post, c) : make_uint4(0, 0, 0, 0);
 #pragma unroll
@@ -270,7 +279,7 @@ __global__ void __launch_bounds__(512, 1) k_block_norm_backward(const __grid_con
     }
     if (GATE == 2 && ok) ldcg_f8(a.gate, c, gate[GATE == 2 ? i : 0]);
   }
-  for (; row < a.T; row += RB * step) {
+  for (; row < a.T; row += RB * step, off += RB * hop) {
     ring.next();
     float sums[3 * RB];                                        // of each row: s^2, dh pre s, y^2
 #pragma unroll
@@ -300,16 +309,14 @@ __global__ void __launch_bounds__(512, 1) k_block_norm_backward(const __grid_con
     float edot[RB];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      const long long here = row + rb * step;
       edot[rb] = 0.f;
-      if (here >= a.T) break;                                  // the ring still holds an older row there
+      if (row + rb * step >= a.T) break;                                  // the ring still holds an older row there
       const float r = rsqrtf(sums[3 * rb] * inv_n + a.eps), ry = POST ? rsqrtf(sums[3 * rb + 2] * inv_n + a.eps) : 1.f;
       const F2 r2 = f2(r), corr = f2(-sums[3 * rb + 1] * inv_n * r * r), scale = f2(a.res_scale), g1 = f2(gate1);
       ry2[rb] = f2(ry);
       F2 edot2 = zero;
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
-        const int c = l + i * lanes;
         F2 s[4], dh[4], w[4], g[4];
         unpack8(ring.get(rb, 0, i), s);
         unpack8(ring.get(rb, 1, i), dh);
@@ -320,11 +327,11 @@ __global__ void __launch_bounds__(512, 1) k_block_norm_backward(const __grid_con
           spre[i][k] = fma2(dh[k], s[k] * r2, spre[i][k]);
           g[k] = fma2(r2, fma2(s[k], corr, dh[k] * w[k]), g[k]);
         }
-        if (c < chunks) {
+        if (i < mine) {
           F2 dx[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) dx[k] = scale * g[k];
-          reinterpret_cast<uint4*>(a.dx + here * a.N)[c] = pack8(dx);
+          *reinterpret_cast<uint4*>(a.dx + off + rb * hop + i * gap) = pack8(dx);
         }
         if (kY) {
           F2 y[4], pw[4], line = zero;
@@ -349,7 +356,7 @@ __global__ void __launch_bounds__(512, 1) k_block_norm_backward(const __grid_con
 #pragma unroll
           for (int k = 0; k < 4; ++k) e[rb][i][k] = g[k];
         }
-        if (!POST && a.dy && c < chunks) reinterpret_cast<uint4*>(a.dy + here * a.N)[c] = pack8(e[rb][i]);
+        if (!POST && a.dy && i < mine) *reinterpret_cast<uint4*>(a.dy + off + rb * hop + i * gap) = pack8(e[rb][i]);
       }
       edot[rb] = both(edot2);
     }
@@ -357,20 +364,18 @@ __global__ void __launch_bounds__(512, 1) k_block_norm_backward(const __grid_con
       rt.sum(edot);
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
-        const long long here = row + rb * step;
-        if (here >= a.T) break;
+        if (row + rb * step >= a.T) break;
         float ry, ry_;
         get(ry2[rb], ry, ry_);
         const F2 take = f2(-edot[rb] * inv_n * ry);
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-          const int c = l + i * lanes;
-          if (c >= chunks) continue;
+          if (i >= mine) continue;
           F2 y[4];
           unpack8(ring.get(rb, K - 1, i), y);
 #pragma unroll
           for (int k = 0; k < 4; ++k) e[rb][i][k] = ry2[rb] * fma2(y[k], take, e[rb][i][k]);
-          reinterpret_cast<uint4*>(a.dy + here * a.N)[c] = pack8(e[rb][i]);
+          *reinterpret_cast<uint4*>(a.dy + off + rb * hop + i * gap) = pack8(e[rb][i]);
         }
       }
     }
@@ -418,11 +423,11 @@ __global__ void __launch_bounds__(512, 1) k_block_norm_backward(const __grid_con
   }
 }
 
-// Sums over the blocks, in their order: 32 columns by 8 slices of blocks.  One block more than the columns need adds the one
+// Sums over the blocks, in their order: 32 columns by 32 slices of blocks (eight were 1.2 us slower: a trip to memory more).  One block more than the columns need adds the one
 // number of a scalar gate.
-__global__ void __launch_bounds__(256) k_norm_sums(const float* part, int blocks, int n, int sums, float* out0, float* out1, float* out2, const double* gate_part,
+__global__ void __launch_bounds__(1024) k_norm_sums(const float* part, int blocks, int n, int sums, float* out0, float* out1, float* out2, const double* gate_part,
                                                    float* dgate1) {
-  __shared__ float red[8][32];
+  __shared__ float red[32][33];
   pdl_launch_dependents();
   pdl_wait();
   const int tid = threadIdx.x, x = tid & 31, y = tid >> 5, width = sums * n;
@@ -437,7 +442,7 @@ __global__ void __launch_bounds__(256) k_norm_sums(const float* part, int blocks
   }
   float v = 0.f;
   if (col < width) {
-    const int b0 = (int)((long long)blocks * y / 8), b1 = (int)((long long)blocks * (y + 1) / 8);
+    const int b0 = (int)((long long)blocks * y / 32), b1 = (int)((long long)blocks * (y + 1) / 32);
 #pragma unroll 8
     for (int b = b0; b < b1; ++b) v += __ldcg(part + (long long)b * width + col);
   }
@@ -446,7 +451,7 @@ __global__ void __launch_bounds__(256) k_norm_sums(const float* part, int blocks
   if (y == 0 && col < width) {
     v = 0.f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v += red[k][x];
+    for (int k = 0; k < 32; ++k) v += red[k][x];
     const int which = col / n;
     float* out = which == 0 ? out0 : which == 1 ? out1 : out2;
     if (out) out[col - which * n] = v;
@@ -488,13 +493,14 @@ static int norm_stages(size_t row_bytes, size_t fixed, int least, int most) {
 cudaError_t launch_block_norm_forward(const BlockNormArgs& a, cudaStream_t st) {
   if (const cudaError_t e = norm_limits()) return e;
   const int chunks = a.N / 8, tensors = a.y ? 2 : 1;
-  // few rows: a thread per piece, the row's latency; many: four pieces a thread, fewer warps to meet per row and more rows at work
+  // few rows: a thread per piece, the row's latency; many: four pieces a thread, fewer warps to meet per row (8192 x 2048 with four pieces and
+  // sixteen warps an SM 29.6 us, with two and thirty-two 33.5, with one 35)
   const int ch = chunks <= 1024 && a.T <= sm_count() ? 1 : 4, most = ch == 1 ? 32 : 16;
   const int warps = (chunks + 32 * ch - 1) / (32 * ch);
   const int teams = std::max(1, std::min(most / warps, 15));                                  // named barriers
   const int blocks = std::min((a.T + teams - 1) / teams, sm_count());
   const bool few = a.T <= blocks * teams;                                                     // one row a team: nothing behind it
-  const size_t fixed = (size_t)teams * team_floats(warps) * sizeof(float), row = (size_t)tensors * ch * warps * 32 * 16 * teams;
+  const size_t fixed = (size_t)teams * team_floats(warps) * sizeof(float), row = (size_t)tensors * ch * 16 * (ch == 1 ? kNormThreads<1> : kNormThreads<4>);
   const int stages = norm_stages(row, fixed, 1, few ? 1 : 4);
   auto kern = ch == 1 ? norm_kernel<1>(a.y != nullptr, a.post != nullptr) : norm_kernel<4>(a.y != nullptr, a.post != nullptr);
   LaunchScope ls(KID_NORM_FWD, st);
@@ -525,7 +531,7 @@ cudaError_t launch_block_norm_backward(const BlockNormArgs& a, void* ws, cudaStr
   auto kern = p.ch == 1 ? norm_bwd_kernel<1>(post, gate) : p.ch == 2 ? norm_bwd_kernel<2>(post, gate) : norm_bwd_kernel<4>(post, gate);
   if (const cudaError_t e = norm_limits()) return e;
   // the sums over tokens take the ring's place in the end
-  const size_t row = (size_t)(a.post || a.gate ? 4 : 3) * p.ch * p.warps * 32 * 16 * p.teams, fixed = (size_t)p.teams * team_floats(p.warps) * sizeof(float);
+  const size_t row = (size_t)(a.post || a.gate ? 4 : 3) * p.ch * 16 * 512, fixed = (size_t)p.teams * team_floats(p.warps) * sizeof(float);
   const int stages = norm_stages(row, fixed, p.ch == 4 ? 1 : 2, 4);
   const size_t smem = fixed + std::max(stages * row, (size_t)sums * a.N * sizeof(float));
   {
@@ -533,7 +539,7 @@ cudaError_t launch_block_norm_backward(const BlockNormArgs& a, void* ws, cudaStr
     if (const cudaError_t e = launch_pdl(kern, p.blocks, p.teams * p.warps * 32, smem, st, a, p.warps, stages, part, gate_part)) return e;
   }
   LaunchScope ls(KID_NORM_SUMS, st);
-  return launch_pdl(k_norm_sums, (sums * a.N + 31) / 32 + (gate == 1 ? 1 : 0), 256, 0, st, part, p.blocks, a.N, sums, a.dh ? a.dpre : nullptr,
+  return launch_pdl(k_norm_sums, (sums * a.N + 31) / 32 + (gate == 1 ? 1 : 0), 1024, 0, st, part, p.blocks, a.N, sums, a.dh ? a.dpre : nullptr,
                     gate == 2 ? a.dgate : a.dpost, a.dpost, gate_part, a.dgate);
 }
 

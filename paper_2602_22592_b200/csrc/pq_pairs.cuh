@@ -3,18 +3,15 @@
 
 namespace pq {
 
-// Pairs of fp32 numbers: one instruction multiplies, adds or both two of them, each rounded as its scalar form rounds.
-struct F2 { uint64_t v; };
-__device__ __forceinline__ F2 f2(float lo, float hi) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi)); return r; }
-__device__ __forceinline__ F2 f2(float x) { return f2(x, x); }
-__device__ __forceinline__ void get(const F2& a, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a.v)); }
-__device__ __forceinline__ F2 operator*(const F2& a, const F2& b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
-__device__ __forceinline__ F2 operator+(const F2& a, const F2& b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
-__device__ __forceinline__ F2 fma2(const F2& a, const F2& b, const F2& c) {
-  F2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-  return r;
-}
-__device__ __forceinline__ float both(const F2& a) { float x, y; get(a, x, y); return x + y; }
+// Pairs of fp32 numbers, as bf16 words unpack into them; every operation rounds each of the two once.  (The packed f32x2 instructions took
+// an eighth fewer instructions and the same time: norms backward of 8192 x 2048 50.4 against 49.9 us.)
+struct F2 { float x, y; };
+__device__ __forceinline__ F2 f2(float lo, float hi) { return F2{lo, hi}; }
+__device__ __forceinline__ F2 f2(float x) { return F2{x, x}; }
+__device__ __forceinline__ void get(const F2& a, float& lo, float& hi) { lo = a.x; hi = a.y; }
+__device__ __forceinline__ F2 operator*(const F2& a, const F2& b) { return F2{__fmul_rn(a.x, b.x), __fmul_rn(a.y, b.y)}; }
+__device__ __forceinline__ F2 operator+(const F2& a, const F2& b) { return F2{__fadd_rn(a.x, b.x), __fadd_rn(a.y, b.y)}; }
+__device__ __forceinline__ F2 fma2(const F2& a, const F2& b, const F2& c) { return F2{__fmaf_rn(a.x, b.x, c.x), __fmaf_rn(a.y, b.y, c.y)}; }
+__device__ __forceinline__ float both(const F2& a) { return a.x + a.y; }
 
 }  // namespace pq
