@@ -28,6 +28,7 @@
 #include <atomic>
 #include <chrono>
 #include <mutex>
+#include <utility>
 
 #include "pq_kernels.cuh"
 
@@ -61,6 +62,16 @@ __device__ __forceinline__ uint32_t attn_place(int r, int c) {
   return r * ROW + ((c ^ (ROW >= 128 ? r & 7 : r >> 1 & 3)) << 4);
 }
 
+// 16 bytes; the offsets are part of the instruction, which spares an addition or two at every copy of a tile
+template <int DST, int SRC>
+__device__ __forceinline__ void attn_copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0+%2], [%1+%3], 16;" ::"r"(dst), "l"(src), "n"(DST), "n"(SRC) : "memory");
+}
+template <bool ALL, int VALUES, int... I>       // the copies of a tile's keys and values that this lane has (32 i < have), or all
+__device__ __forceinline__ void attn_copy_tile(std::integer_sequence<int, I...>, uint32_t dst, const uint32_t* place, const void* kp, const void* vp, int have) {
+  ([&] { if (ALL || 32 * I < have) attn_copy16<0, 512 * I>(dst + place[I], kp); }(), ...);
+  ([&] { if (ALL || 32 * I < have) attn_copy16<VALUES, 512 * I>(dst + place[I], vp); }(), ...);
+}
 __device__ __forceinline__ void attn_copy4(uint32_t dst, const void* src, bool valid) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(valid ? 4 : 0) : "memory");
 }
@@ -356,13 +367,11 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
         const uint8_t* const vp = static_cast<const uint8_t*>(a.c.V) + row0 * row_bytes + lane * 16;
         const uint32_t dst = ring_at + stage * F::kStageBytes;
         const int have = min(rows, kAttnTile) * chunks - lane;            // this lane's pieces: 32 i < have
-        if (rows >= kAttnTile) {
-#pragma unroll
-          for (int i = 0; i < F::kCopies; ++i)
-            if (32 * i < have) cp_async16(dst + place[i], kp + 512 * i, true);
-#pragma unroll
-          for (int i = 0; i < F::kCopies; ++i)
-            if (32 * i < have) cp_async16(dst + F::kTileBytes + place[i], vp + 512 * i, true);
+        using Copies = std::make_integer_sequence<int, F::kCopies>;
+        if (rows >= kAttnTile && chunks == F::kChunks) {
+          attn_copy_tile<true, F::kTileBytes>(Copies{}, dst, place, kp, vp, have);
+        } else if (rows >= kAttnTile) {
+          attn_copy_tile<false, F::kTileBytes>(Copies{}, dst, place, kp, vp, have);
         } else {                                              // the sequence ends inside: rows behind its end are zero, and not read
 #pragma unroll
           for (int i = 0; i < F::kCopies; ++i)

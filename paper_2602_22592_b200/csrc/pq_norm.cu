@@ -34,6 +34,7 @@ __device__ __forceinline__ void ldcg_f8(const float* p, int chunk, F2 (&v)[4]) {
   const float4 a = __ldcg(reinterpret_cast<const float4*>(p) + 2 * chunk), b = __ldcg(reinterpret_cast<const float4*>(p) + 2 * chunk + 1);
   v[0] = f2(a.x, a.y); v[1] = f2(a.z, a.w); v[2] = f2(b.x, b.y); v[3] = f2(b.z, b.w);
 }
+__device__ __forceinline__ void norm_copy16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
 template <int N>
 __device__ __forceinline__ void norm_copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void norm_copy_wait(int pending) {
@@ -75,7 +76,7 @@ struct RowRing {
         if (!from[k]) continue;
 #pragma unroll
         for (int i = 0; i < CH; ++i)
-          if (i < mine) cp_async16(dst + (k * CH + i) * kPiece, from[k] + i * gap, true);
+          if (i < mine) norm_copy16(dst + (k * CH + i) * kPiece, from[k] + i * gap);
         from[k] += hop;
       }
       --left;
