@@ -739,14 +739,14 @@ int pq_kv_append(const pq_kv_cache* c, int tokens, const int32_t* seq, const int
                  int q_heads, uint16_t* Q_out, void* stream) {
   KvCache kv;
   if (const int rc = check_kv(c, &kv)) return rc;
+  if (tokens <= 0) return tokens == 0 ? PQ_OK : PQ_ERR_SHAPE;
   if (!seq || !pos || !K || !V || !cos != !sin || !Q != !Q_out) return PQ_ERR_NULL;
-  if (tokens < 0 || q_heads < 0 || (q_heads > 0) != (Q != nullptr) || q_heads > INT32_MAX / 512 || (cos && rope_rows < 1)) return PQ_ERR_SHAPE;
+  if (q_heads < 0 || (q_heads > 0) != (Q != nullptr) || q_heads > INT32_MAX / 512 || (cos && rope_rows < 1)) return PQ_ERR_SHAPE;
   const int64_t dense = (int64_t)kv.heads * kv.dim, q_dense = (int64_t)q_heads * kv.dim;
   if (!row_stride(k_stride, dense, &k_stride) || !row_stride(v_stride, dense, &v_stride) || (Q && !row_stride(q_stride, q_dense, &q_stride))) return PQ_ERR_SHAPE;
   if (Q && Q_out == Q && q_stride != q_dense) return PQ_ERR_SHAPE;      // rows of the output would lie over other rows of the input
   if (misaligned(seq) || misaligned(pos) || misaligned(K) || misaligned(V) || misaligned(cos) || misaligned(sin) || misaligned(Q) || misaligned(Q_out))
     return PQ_ERR_ALIGN;
-  if (tokens == 0) return PQ_OK;
   return launch_kv_append(kv, tokens, seq, pos, K, k_stride, V, v_stride, cos, sin, rope_rows, Q, q_stride, q_heads, Q_out,
                           static_cast<cudaStream_t>(stream)) == cudaSuccess ? PQ_OK : PQ_ERR_CUDA;
 }
@@ -754,10 +754,9 @@ int pq_kv_append(const pq_kv_cache* c, int tokens, const int32_t* seq, const int
 int pq_kv_read(const pq_kv_cache* c, int tokens, const int32_t* seq, const int32_t* pos, uint16_t* K_out, uint16_t* V_out, void* stream) {
   KvCache kv;
   if (const int rc = check_kv(c, &kv)) return rc;
+  if (tokens <= 0) return tokens == 0 ? PQ_OK : PQ_ERR_SHAPE;
   if (!seq || !pos || !K_out || !V_out) return PQ_ERR_NULL;
-  if (tokens < 0) return PQ_ERR_SHAPE;
   if (misaligned(seq) || misaligned(pos) || misaligned(K_out) || misaligned(V_out)) return PQ_ERR_ALIGN;
-  if (tokens == 0) return PQ_OK;
   return launch_kv_read(kv, tokens, seq, pos, K_out, V_out, static_cast<cudaStream_t>(stream)) == cudaSuccess ? PQ_OK : PQ_ERR_CUDA;
 }
 

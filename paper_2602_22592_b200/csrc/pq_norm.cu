@@ -499,7 +499,7 @@ cudaError_t launch_block_norm_forward(const BlockNormArgs& a, cudaStream_t st) {
   const int ch = chunks <= 1024 && a.T <= sm_count() ? 1 : 4, most = ch == 1 ? 32 : 16;
   const int warps = (chunks + 32 * ch - 1) / (32 * ch);
   const int teams = std::max(1, std::min(most / warps, 15));                                  // named barriers
-  const int blocks = std::min((a.T + teams - 1) / teams, sm_count());
+  const int blocks = (int)std::min<long long>(((long long)a.T + teams - 1) / teams, sm_count());
   const bool few = a.T <= blocks * teams;                                                     // one row a team: nothing behind it
   const size_t fixed = (size_t)teams * team_floats(warps) * sizeof(float), row = (size_t)tensors * ch * 16 * (ch == 1 ? kNormThreads<1> : kNormThreads<4>);
   const int stages = norm_stages(row, fixed, 1, few ? 1 : 4);
@@ -515,7 +515,7 @@ static NormBwdPlan norm_bwd_plan(int T, int N) {
   p.ch = chunks <= 256 ? 1 : chunks <= 1024 ? 2 : 4;           // two rows at work in a block as long as they fit
   p.warps = (chunks + 32 * p.ch - 1) / (32 * p.ch);
   p.teams = std::max(1, std::min(16 / p.warps, 15));           // named barriers
-  p.blocks = std::min(sm_count(), (T + p.teams - 1) / p.teams);
+  p.blocks = (int)std::min<long long>(sm_count(), ((long long)T + p.teams - 1) / p.teams);
   return p;
 }
 size_t block_norm_workspace_bytes(int T, int N) {

@@ -162,6 +162,7 @@ def test_cache_refusals(lib):
             assert call(cache(lib, **bad)) == lib.PQ_ERR_SHAPE, bad
     # tokens: none is a call that does nothing, fewer is an error
     assert append(good, tokens=0) == lib.PQ_OK and read(good, tokens=0) == lib.PQ_OK
+    assert append(good, tokens=0, seq=None, pos=None, K=None, V=None) == lib.PQ_OK and read(good, tokens=0, seq=None, pos=None, K=None, V=None) == lib.PQ_OK
     assert append(good, tokens=-1) == lib.PQ_ERR_SHAPE and read(good, tokens=-1) == lib.PQ_ERR_SHAPE
     for name in ("seq", "pos", "K", "V"):
         assert append(good, **{name: None}) == lib.PQ_ERR_NULL and append(good, **{name: P + 4}) == lib.PQ_ERR_ALIGN

@@ -471,6 +471,82 @@ def test_repeated_calls_give_the_same_bits():
     assert all(torch.equal(o, outs[0]) for o in outs)
 
 
+def test_sequences_that_share_pages():
+    # two sequences with the first pages of a third: they see the same rows, and rows written to their own pages stay theirs
+    rng = np.random.default_rng(28)
+    C = Cache(rng, [48, 16, 16], 2, 64, 16, False, width=4)
+    rows = C.fill(rng, [48, 16, 16])
+    table = C.table_host.copy()
+    own = [table[1, 0], table[2, 0]]
+    for s in (1, 2):
+        table[s, :3], table[s, 3] = table[0, :3], own[s - 1]
+    C.table.copy_(torch.from_numpy(table))
+    lens = [48, 56, 33]
+    seen = [rows[0], [np.concatenate([rows[0][w], rows[1][w][:8]]) for w in range(2)], [rows[0][w][:33] for w in range(2)]]
+    q = B.bf16(rng.standard_normal((3, 4, 64)))
+    O = torch.empty((3, 256), dtype=torch.bfloat16, device=DEV)
+    ws = torch.empty(pqb.pq_attn_workspace_bytes(C.c, 4), dtype=torch.uint8, device=DEV)
+    pqb.pq_attn_decode(C.c, bf(q).view(3, -1), torch.tensor(lens, dtype=torch.int32, device=DEV), 0.125, O, None, ws)
+    check_status()
+    close_attention(O, None, q, seen, 0.125)
+
+
+@pytest.mark.parametrize("int8", [False, True])
+def test_a_value_that_is_not_a_number_reaches_its_own_outputs(int8):
+    rng = np.random.default_rng(29)
+    C = Cache(rng, [40, 40], 2, 64, 16, int8)
+    rows = C.fill(rng, [40, 40])
+    pg, at = C.table_host[0, 1], 5                 # position 21 of sequence 0, head 1
+    if int8:
+        C.vg[pg, 1, at] = float("nan")             # the whole row
+    else:
+        C.v[pg, 1, at, 7] = float("nan")
+    q = B.bf16(rng.standard_normal((2, 2, 64)))
+    O = torch.empty((2, 128), dtype=torch.bfloat16, device=DEV)
+    ws = torch.empty(pqb.pq_attn_workspace_bytes(C.c, 2), dtype=torch.uint8, device=DEV)
+    pqb.pq_attn_decode(C.c, bf(q).view(2, -1), torch.tensor([40, 40], dtype=torch.int32, device=DEV), 0.125, O, None, ws)
+    check_status()
+    nan = torch.isnan(O).view(2, 2, 64).cpu()
+    want = torch.zeros((2, 2, 64), dtype=torch.bool)
+    want[0, 1] = True if int8 else torch.arange(64) == 7
+    assert torch.equal(nan, want)
+    close_attention(O[1:], None, q[1:], rows[1:], 0.125, int8)
+
+
+def test_two_threads_attend_on_their_own_streams():
+    # one cache, two host threads with streams, queries and workspaces of their own: each call's result is the one it has alone
+    import threading
+    rng = np.random.default_rng(30)
+    lens = [int(x) for x in rng.integers(1, 1500, 12)]
+    C = Cache(rng, lens, 4, 128, 32, False)
+    C.fill(rng, lens)
+    lt = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    qs = [bf(rng.standard_normal((12, 512))) for _ in range(2)]
+    new = lambda: torch.empty((12, 512), dtype=torch.bfloat16, device=DEV)  # noqa: E731
+    wss = [torch.full((pqb.pq_attn_workspace_bytes(C.c, 4),), 255 * i, dtype=torch.uint8, device=DEV) for i in range(2)]
+    want = [new(), new()]
+    for i in range(2):
+        pqb.pq_attn_decode(C.c, qs[i], lt, 0.1, want[i], None, wss[i])
+    torch.cuda.synchronize()
+    outs, errors = [[], []], []
+
+    def work(i):
+        try:
+            st = torch.cuda.Stream()
+            with torch.cuda.stream(st):
+                for _ in range(50):
+                    outs[i].append(new())
+                    pqb.pq_attn_decode(C.c, qs[i], lt, 0.1, outs[i][-1], None, wss[i])
+            st.synchronize()
+        except Exception as e:      # pragma: no cover
+            errors.append(e)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    check_status()
+    assert not errors and all(torch.equal(o, want[i]) for i in range(2) for o in outs[i])
+
+
 # --------------------------------------------------------------------------- norms
 def norm_case(rng, T, N, post, gate):
     x, y = B.bf16(rng.standard_normal((T, N)) * 2), B.bf16(rng.standard_normal((T, N)))
