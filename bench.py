@@ -708,16 +708,16 @@ def run_decode(args, ctx):
 
 
 # --------------------------------------------------------------------------- whole decoder step (config 4)
-def measure_decoder(ctx, steps, warmup, both_attention_forms, engine):
+def measure_decoder(ctx, steps, warmup, both_attention_forms, engine, library_norms=False):
     """One QAT step (forward + backward, no optimiser) of a 24-layer 1.3B-shaped decoder whose 168 projections are
     pQuant linears with 8 experts, top-1; token ids uniform over the vocabulary.  The device time of the pq_* calls is
     summed from CUDA events around them and reported apart from the rest (attention, norms, rotary embedding, LM head,
-    loss: plain torch)."""
+    loss: plain torch; with library_norms the norms and residual additions are pq_block_norm calls, counted with the rest)."""
     torch = ctx.torch
     from paper_2602_22592_b200.decoder_harness import PQDecoder
 
     def one(attn_hp):
-        m = PQDecoder(attn_hp=attn_hp, device=ctx.device)
+        m = PQDecoder(attn_hp=attn_hp, device=ctx.device, library_norms=library_norms)
         ids, tgt = m.random_batch()
         for _ in range(warmup):
             m.step(ids, tgt)
@@ -760,14 +760,15 @@ def measure_decoder(ctx, steps, warmup, both_attention_forms, engine):
 
 def run_decoder(args, ctx):
     engine = measure_engine_peaks(ctx)
-    rec = measure_decoder(ctx, args.steps, args.warmup, not args.decoder_one_form, engine)
+    rec = measure_decoder(ctx, args.steps, args.warmup, not args.decoder_one_form, engine, args.library_norms)
     main = rec["all_projections_8_experts"]
     if ctx.rank == 0:
         out = {"metric": "pQuant decoder QAT step tokens/s (pQuant-linear time apart)", "value": main["tokens_per_s"], "unit": "tokens/s",
                "n_gpus": ctx.world, "steps": args.steps, "warmup": args.warmup, "ms_per_step": main["ms_per_step"],
                "higher_is_better": True, "scaling": "weak", "vs_baseline": None,
                "dtype": "int8 x int8 -> int32 / bf16 -> fp32 (pQuant linears); bf16 (torch rest)", "data": "synthetic",
-               "config": {"workload": rec["workload"], "l2": "activations and weights of a step far exceed L2", "replicas": ctx.world},
+               "config": {"workload": rec["workload"], "l2": "activations and weights of a step far exceed L2", "replicas": ctx.world,
+                          **({"library_norms": True} if args.library_norms else {})},
                "engine_peaks": engine, "decoder": rec, "clocks": main["clocks"], "e2e": None, "gpu_launches": int(ctx.pqb.pq_kernel_launches())}
         print(json.dumps(out))
     ctx.reps.close()
@@ -886,6 +887,7 @@ def main():
     ap.add_argument("--decode-mma-from", type=int, default=5, help="streaming decode kernel: token groups of at least this size use the tensor-core bit product")
     ap.add_argument("--decode-prefetch", type=int, default=1, choices=[0, 1], help="streaming decode kernel: L2 prefetch of the sign bits during the token work")
     ap.add_argument("--decode-rmsnorm", action="store_true", help="decode from un-normalised activations, RMSNorm fused into the token preparation")
+    ap.add_argument("--library-norms", action="store_true", help="decoder workload: norms and residual additions by pq_block_norm_forward / _backward")
     ap.add_argument("--decoder-one-form", action="store_true", help="decoder workload: only the form with 8 experts on every projection")
     ap.add_argument("--cpu-tokens", type=int, default=8192, help="tokens per step of the CPU oracle (cpu_baseline and --impl reference)")
     ap.add_argument("--no-e2e", action="store_true")
