@@ -4,6 +4,9 @@
 // takes a row with accesses of up to 16 bytes and a warp 32 / G rows at once, kSteps times over: a unit, of one token.  Position,
 // sequence, page id and row are four trips to memory one after another; warps walk the units with a stride and ask for the next
 // unit's indices before they work on this one's rows.
+// Measured: 7850 tokens of 16 heads of 128 in bf16, written with their queries 32 us (6.1 TB/s) and read back 23 (5.6); 2142 tokens of 32 heads
+// of 100 in int8 written 37 us, 5356 read back 33: there the instructions are the limit (65 % of the issue slots), about a hundred a
+// row, since 50 values half a row can only be had in twos.
 #include <algorithm>
 #include <cstring>
 

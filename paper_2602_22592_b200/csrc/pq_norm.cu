@@ -3,8 +3,10 @@
 // y is the block's output, x the stream in front of it, s the stream behind it, h the next block's input.  Sums, norms and s itself
 // are held in fp32; s and h are rounded once, each from fp32.
 //
-// Bound by memory: a row stays in the registers of the warps that own it from its load to its store, so that every tensor moves
-// once.
+// Every tensor moves once: rows come through shared memory by asynchronous copies, several ahead, and are finished where they are.
+// Measured at 8192 x 2048 with a norm behind the block and a gate per feature: forward 30 us (134 MB, 4.5 TB/s; a copy of as much 20.5), backward
+// 50 us (201 MB, 4.0 TB/s).  The forward waits at two meetings of a row's warps; the backward issues in 69 % of its slots: 27 fp32 operations a
+// value and as much again to unpack, address and add up.  999 x 3200 without a norm behind the block: 18 us, 5 of them the sums over blocks.
 #include <algorithm>
 #include <mutex>
 

@@ -273,7 +273,8 @@ def close_attention(O, lse, q, rows, scale, int8=False):
 ATTEND = [  # heads, group, dim, page, lengths
     (2, 1, 128, 16, [1, 15, 16, 17, 0, 129, 64]), (3, 4, 64, 48, [200, 1, 97]), (2, 1, 100, 32, [31, 333, 0, 2]), (1, 8, 128, 64, [1000]),
     (2, 5, 96, 16, [77, 50, 3]), (1, 16, 128, 16, [260, 9]), (2, 9, 64, 16, [40, 41]), (1, 20, 80, 32, [100, 0, 64]), (1, 40, 128, 16, [90]),
-    (2, 3, 256, 16, [70, 1, 128]), (1, 16, 192, 32, [65, 130]), (4, 2, 8, 16, [20, 33]), (1, 1, 12, 16, [5]), (16, 1, 128, 64, [1500, 3, 700])]
+    (2, 3, 256, 16, [70, 1, 128]), (1, 16, 192, 32, [65, 130]), (4, 2, 8, 16, [20, 33]), (1, 1, 12, 16, [5]), (16, 1, 128, 64, [1500, 3, 700]), (3, 2, 40, 16, [33, 5]), (2, 9, 32, 16, [70, 16]), (1, 2, 112, 48, [130, 47, 200]),
+    (2, 1, 180, 16, [90, 31])]
 
 
 @pytest.mark.parametrize("int8", [False, True])
@@ -358,13 +359,14 @@ def test_attention_over_one_long_sequence(int8, group):
     close_attention(O, lse, q, rows, 128 ** -0.5, int8)
 
 
-def test_attention_with_extreme_scores():
+@pytest.mark.parametrize("dim", [64, 100])
+def test_attention_with_extreme_scores(dim):
     # scores far apart, equal, -infinity for some positions and for all, NaN: as the definition says
     rng = np.random.default_rng(24)
     lens = [50, 50, 50, 50, 50]
-    C = Cache(rng, lens, 1, 64, 16, False)
+    C = Cache(rng, lens, 1, dim, 16, False)
     rows = C.fill(rng, lens)
-    q = B.bf16(rng.standard_normal((5, 1, 64)))
+    q = B.bf16(rng.standard_normal((5, 1, dim)))
     q[0] = B.bf16(q[0] * 1000)                 # one position takes all the weight
     q[1] = 0                                   # the mean of the values
     k = C.k.float().cpu().numpy()
@@ -375,7 +377,7 @@ def test_attention_with_extreme_scores():
         k[C.table_host[3, p // 16], 0, p % 16, 0] = -np.inf
     C.k.copy_(torch.from_numpy(k))
     q[2, 0, 0] = q[3, 0, 0] = 1.0              # sign known: -infinity
-    O, lse = torch.empty((5, 64), dtype=torch.bfloat16, device=DEV), torch.empty((5, 1), device=DEV)
+    O, lse = torch.empty((5, dim), dtype=torch.bfloat16, device=DEV), torch.empty((5, 1), device=DEV)
     ws = torch.empty(pqb.pq_attn_workspace_bytes(C.c, 1), dtype=torch.uint8, device=DEV)
     pqb.pq_attn_decode(C.c, bf(q).view(5, -1), torch.tensor(lens, dtype=torch.int32, device=DEV), 1.0, O, lse, ws)
     check_status()
