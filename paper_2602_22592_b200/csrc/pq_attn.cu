@@ -43,7 +43,7 @@ namespace pq {
 
 constexpr int kAttnTile = 16;                 // positions of a tile; pages are multiples of it
 constexpr int kAttnRingBytes = 204 * 1024;    // of 227 KB a CTA can have, 18 of them static
-constexpr int kAttnSmemMost = 209 * 1024;
+constexpr int kAttnSmemMost = 209 * 1024;     // what a launch can ask for beside them
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
 template <int DP, int NT, bool I8>
@@ -232,19 +232,19 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const int per_seq = a.by_per_seq.d, n = a.c.num_seqs, row_bytes = a.c.pitch * (I8 ? 1 : 2), chunks = row_bytes / 16;
   uint8_t* const ring = smem + warp * (F::kStages * F::kStageBytes);
-      // copy i takes this lane's piece 32 i + lane of the tile, whose rows are neighbours in the page
-      uint32_t place[F::kCopies];
-  #pragma unroll
-      for (int i = 0; i < F::kCopies; ++i) {
-        const int at = 32 * i + lane, r = a.by_chunks(at);
-        place[i] = attn_place<F::kRow>(r, at - r * chunks);
-      }
-      if (chunks < F::kChunks) {                                // pieces behind the rows' end are never copied: zeros once and for all
-        for (int s = 0; s < F::kStages; ++s)
-          for (int i = lane; i < kAttnTile * F::kChunks; i += 32)
-            if (i % F::kChunks >= chunks)
-              *reinterpret_cast<uint4*>(ring + s * F::kStageBytes + attn_place<F::kRow>(i / F::kChunks, i % F::kChunks)) = make_uint4(0, 0, 0, 0);
-      }
+  // copy i takes this lane's piece 32 i + lane of the tile, whose rows are neighbours in the page
+  uint32_t place[F::kCopies];
+#pragma unroll
+  for (int i = 0; i < F::kCopies; ++i) {
+    const int at = 32 * i + lane, r = a.by_chunks(at);
+    place[i] = attn_place<F::kRow>(r, at - r * chunks);
+  }
+  if (chunks < F::kChunks) {                                // pieces behind the rows' end are never copied: zeros once and for all
+    for (int s = 0; s < F::kStages; ++s)
+      for (int i = lane; i < kAttnTile * F::kChunks; i += 32)
+        if (i % F::kChunks >= chunks)
+          *reinterpret_cast<uint4*>(ring + s * F::kStageBytes + attn_place<F::kRow>(i / F::kChunks, i % F::kChunks)) = make_uint4(0, 0, 0, 0);
+  }
   // lengths, page ids and queries are trips to memory one after another: ask for them to be in L2 (where later writes reach them too)
   {
     const long long line = (long long)(blockIdx.x * kThreads + tid) * 128;
@@ -350,7 +350,7 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
     // page ids of the sequence, a window of 32 at a time: lane i holds the one of page window + i
     int window = a.by_page_tiles(pt), ids;
     auto ask = [&]() {
-      const int at = window + lane, most = (pw.len + a.c.page_size - 1) / a.c.page_size;
+      const int at = window + lane, most = a.by_page_tiles(pw.tiles - 1) + 1;
       ids = at < most ? __ldcg(a.c.page_table + (long long)pw.seq * a.c.max_pages + at) : -1;
     };
     ask();
@@ -842,11 +842,11 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
 // host side
 // ---------------------------------------------------------------------------
 using AttnKernel = void (*)(AttnArgs);
-struct AttnChoice { AttnKernel kernel; int smem, warps, most; };     // rings; and what a CTA can ask for at most beside its static share
+struct AttnChoice { AttnKernel kernel; int smem, warps; };
 template <int DP, int NT>
 static AttnChoice attn_choice(bool i8) {
-  return i8 ? AttnChoice{k_attn_decode<DP, NT, true>, AttnForm<DP, NT, true>::kSmem, AttnForm<DP, NT, true>::kWarps, kAttnSmemMost}
-            : AttnChoice{k_attn_decode<DP, NT, false>, AttnForm<DP, NT, false>::kSmem, AttnForm<DP, NT, false>::kWarps, kAttnSmemMost};
+  return i8 ? AttnChoice{k_attn_decode<DP, NT, true>, AttnForm<DP, NT, true>::kSmem, AttnForm<DP, NT, true>::kWarps}
+            : AttnChoice{k_attn_decode<DP, NT, false>, AttnForm<DP, NT, false>::kSmem, AttnForm<DP, NT, false>::kWarps};
 }
 static AttnChoice attn_choice(int dp, int nt, bool i8) {
   if (dp == 64) return nt == 1 ? attn_choice<64, 1>(i8) : attn_choice<64, 2>(i8);
@@ -903,7 +903,7 @@ static cudaError_t attn_limits() {
         for (int i8 = 0; i8 < 2; ++i8) {
           if (result[dev] != cudaSuccess) return;
           const AttnChoice ch = attn_choice(dp, nt, i8);
-          result[dev] = cudaFuncSetAttribute(ch.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ch.most);
+          result[dev] = cudaFuncSetAttribute(ch.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmemMost);
         }
   });
   return result[dev];
@@ -922,7 +922,7 @@ cudaError_t launch_attn_decode(const KvCache& c, int q_heads, const uint16_t* Q,
   a.by_page_tiles = FastDiv(c.page_size / kAttnTile);
   a.by_chunks = FastDiv(c.pitch * (c.format == PQ_KV_INT8 ? 1 : 2) / 16);
   const size_t firsts = (size_t)p.choice.warps * std::min(a.group, 8 * p.nt) * p.dp * 4;
-  a.first_in_smem = p.choice.smem + firsts <= (size_t)p.choice.most;
+  a.first_in_smem = p.choice.smem + firsts <= (size_t)kAttnSmemMost;
   a.call = attn_call_number();
   attn_carve(p, ws, &a);
   LaunchScope ls(KID_ATTN_DECODE, st);
