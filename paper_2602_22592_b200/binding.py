@@ -424,11 +424,12 @@ def _at(fn, name, t, dtype, numel, dev):
 
 
 def _rows_at(fn, name, t, rows, width, dev):
-    """Address and row stride in values (0: dense) of `rows` rows of `width` bf16 values, each of them contiguous."""
+    """Address and row stride in values (0: dense) of `rows` rows of `width` bf16 values, each of them contiguous.  A broadcast row is
+    refused: its stride of 0 would mean dense rows."""
     if t.is_contiguous():
         return _at(fn, name, t, torch.bfloat16, rows * width, dev), 0
-    if t.dtype is not torch.bfloat16 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width or t.stride(1) != 1:
-        raise PqArgumentError(fn, f"{name} has to hold {rows} rows of {width} bfloat16 values, each of them contiguous")
+    if t.dtype is not torch.bfloat16 or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width or t.stride(1) != 1 or t.stride(0) < width:
+        raise PqArgumentError(fn, f"{name} has to hold {rows} rows of {width} bfloat16 values, each of them contiguous and apart from the others")
     if t.get_device() != dev:
         raise PqArgumentError(fn, f"{name} is on {t.device}, the current device is cuda:{dev}")
     return t.data_ptr(), t.stride(0) if rows > 1 else 0      # the stride of a single row means nothing

@@ -245,3 +245,12 @@ def test_binding_checks_types_shapes_and_layouts(lib):
     with pytest.raises(lib.PqArgumentError):
         lib._whole("f", "x", t(5, 64), 100)
     assert lib._at("f", "x", None, torch.int32, 7, 0) is None
+
+
+def test_rows_that_lie_on_one_another_are_refused(lib):
+    # one row for all (stride 0, which the library takes for dense rows: they would be read far behind the tensor's end) and overlapping ones
+    one = torch.zeros(64, dtype=torch.bfloat16)
+    for bad in (one.expand(5, 64), one[None].expand(5, 64), torch.zeros(320, dtype=torch.bfloat16).as_strided((5, 64), (32, 1))):
+        with pytest.raises(lib.PqArgumentError):
+            lib._rows_at("f", "x", bad, 5, 64, -1)
+    assert lib._rows_at("f", "x", one.expand(1, 64), 1, 64, -1)[1] == 0
