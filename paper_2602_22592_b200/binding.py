@@ -492,6 +492,8 @@ def pq_kv_append(cache, seq, pos, K, V, cos=None, sin=None, Q=None, Q_out=None, 
         if cos is None or sin is None:
             raise PqArgumentError(fn, "cos and sin come together")
         rope_rows = _whole(fn, "cos", cos, dim // 2)
+        if not rope_rows:      # an empty tensor has no address, and without one nothing would be rotated
+            raise PqArgumentError(fn, "cos has no rows")
         c, d = _at(fn, "cos", cos, torch.float32, rope_rows * (dim // 2), dev), _at(fn, "sin", sin, torch.float32, rope_rows * (dim // 2), dev)
     if Q is not None or Q_out is not None:
         if Q is None or Q_out is None:

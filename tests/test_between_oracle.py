@@ -254,3 +254,17 @@ def test_rows_that_lie_on_one_another_are_refused(lib):
         with pytest.raises(lib.PqArgumentError):
             lib._rows_at("f", "x", bad, 5, 64, -1)
     assert lib._rows_at("f", "x", one.expand(1, 64), 1, 64, -1)[1] == 0
+
+
+def test_empty_rotary_tables_are_refused(lib, monkeypatch):
+    # an empty tensor has no address, which the library takes for a call without a rotation
+    monkeypatch.setattr(lib, "_device", lambda: -1)
+    cache = lib.make_kv_cache(torch.zeros(2, 1, 16, 64, dtype=torch.bfloat16), torch.zeros(2, 1, 16, 64, dtype=torch.bfloat16),
+                              torch.zeros(1, 2, dtype=torch.int32), 64)
+    row, at = torch.zeros(1, 64, dtype=torch.bfloat16), torch.zeros(1, dtype=torch.int32)
+    empty = torch.zeros(0, 32)
+    monkeypatch.setattr(lib, "_stream", lambda s: None)
+    monkeypatch.setattr(lib, "_check", lambda fn, status: pytest.fail("the call went through"))
+    monkeypatch.setattr(lib, "lib", lambda: type("L", (), {"pq_kv_append": staticmethod(lambda *a: 0)}))
+    with pytest.raises(lib.PqArgumentError):
+        lib.pq_kv_append(cache, at, at, row, row, empty, empty)
