@@ -18,8 +18,9 @@
 //     rows of V^T are permuted accordingly, queries and outputs with them.
 //   * Types of the products.  A bf16 cache multiplies in bf16, and the weights enter the second product as the sum of two bf16
 //     numbers (2^-16 relative at most): a single rounding of them would be as large as the output's own.  An int8 cache multiplies in
-//     fp16, where codes are exact and cost least to make: queries are scaled by a power of two per row (exact: bf16 has
-//     fewer bits), and the weights, 2^14 at most, are rounded once to eleven bits, an eighth of the output's rounding.  gamma_k
+//     fp16, where codes are exact and cost least to make: queries are scaled by a power of two per row (exact down to 2^-32 of the row's
+//     largest: bf16 has fewer bits), and the weights, 2^14 at most, enter as the sum of two fp16 numbers, 2^-22 relative down to 2^-17 of
+//     the largest and 2^-39 of the largest below that.  (One number, 2^-11, shows where values cancel.)  gamma_k
 //     scales the scores; the weights are taken with their 1 / gamma_v inside the exponent, exp2(s - log2 gamma_v - m), m the
 //     maximum of that, so that they stay in range, and the sum of weights puts gamma_v back.
 // Measured (us, GB/s of the cache): sixty-four ragged sequences of up to 4096 positions, eight heads of 128 with four query heads each, bf16
@@ -578,7 +579,10 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             if constexpr (I8) {
-              ph[nt][h] = transpose8x8(pack_f16x2(p[2 * h], p[2 * h + 1]));
+              const uint32_t hi = pack_f16x2(p[2 * h], p[2 * h + 1]);
+              const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+              ph[nt][h] = transpose8x8(hi);
+              pl[nt][h] = transpose8x8(pack_f16x2(p[2 * h] - back.x, p[2 * h + 1] - back.y));
             } else {
               const uint32_t hi = pack_bf16x2(p[2 * h], p[2 * h + 1]);
               ph[nt][h] = transpose8x8(hi);
@@ -596,7 +600,10 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
               const uint32_t x0 = w[2 * h] ^ 0x80808080u, x1 = w[2 * h + 1] ^ 0x80808080u;
               const uint32_t a0 = codes_pair<0x4240>(x0), a1 = codes_pair<0x4341>(x0), a2 = codes_pair<0x4240>(x1), a3 = codes_pair<0x4341>(x1);
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][2 * j + h], a0, a1, a2, a3, ph[nt][0], ph[nt][1]);
+              for (int nt = 0; nt < NT; ++nt) {
+                mma_f16(o[nt][2 * j + h], a0, a1, a2, a3, ph[nt][0], ph[nt][1]);
+                mma_f16(o[nt][2 * j + h], a0, a1, a2, a3, pl[nt][0], pl[nt][1]);
+              }
             }
           } else {
 #pragma unroll

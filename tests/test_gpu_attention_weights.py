@@ -1,0 +1,60 @@
+"""How far the weights of pq_attn_decode are off, seen where nothing else is: values that cancel, values far apart, infinities.
+
+Tolerances count roundings.  Relative errors of one weight: exp2 2^-22, the reciprocal of an int8 row's gamma 2^-23, products and
+differences in fp32 2^-24 each; of an int8 cache two fp16 numbers, 2^-11 2^-11 = 2^-22.  A sum inside a tensor core may cut each of its
+17 terms at 2^-23 of the largest one.  Together W = 2^-18 of sum |p v| / sum p for a handful of positions (2^-22 + 2^-23 + 4 2^-24 + 2^-22 +
+17 2^-23 = 2^-18.6); a score's error is counted apart."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import between_oracle as B
+from paper_2602_22592_b200 import binding as pqb
+from test_gpu_between import DEV, HALF, Cache, bf, check_status, f64
+
+pytestmark = pytest.mark.gpu
+W = 2.0 ** -18
+
+
+def attend(C, q, lens, scale, lse=None):
+    n, H = q.shape[:2]
+    O = torch.empty((n, q.shape[1] * q.shape[2]), dtype=torch.bfloat16, device=DEV)
+    ws = torch.full((pqb.pq_attn_workspace_bytes(C.c, H),), 255, dtype=torch.uint8, device=DEV)
+    pqb.pq_attn_decode(C.c, bf(q).view(n, -1), torch.tensor(lens, dtype=torch.int32, device=DEV), scale, O, lse, ws)
+    check_status()
+    return f64(O).reshape(q.shape)
+
+
+@pytest.mark.parametrize("dim,group", [(8, 1), (64, 12), (128, 1), (128, 12), (256, 3)])
+def test_int8_weights_where_values_cancel(dim, group):
+    # two positions a sequence whose first values cancel: gamma_v of the second is chosen for it (to fp32's rounding), so that the
+    # output there is the weights' own error
+    rng = np.random.default_rng(41)
+    n, scale = 48, 0.25
+    C = Cache(rng, [2] * n, 1, dim, 16, True)
+    rows = C.fill(rng, [2] * n)
+    k, v = C.k.cpu().numpy(), C.v.cpu().numpy()
+    kg, vg = C.kg.cpu().numpy(), C.vg.cpu().numpy()
+    q = np.zeros((n, group, dim))
+    q[:, :, 0] = 1
+    for s in range(n):
+        pg = C.table_host[s, 0]
+        k[pg, 0, :2] = 0
+        k[pg, 0, :2, 0] = rng.integers(-128, 128, 2)
+        kg[pg, 0, :2] = rng.uniform(60, 250, 2).astype(np.float32)
+        keys = k[pg, 0, :2].astype(np.float64) / kg[pg, 0, :2].astype(np.float64)[:, None]
+        p = np.exp(scale * keys[:, 0])
+        a, b = rng.integers(60, 128), -rng.integers(60, 128)
+        v[pg, 0, 0, 0], v[pg, 0, 1, 0] = a, b
+        vg[pg, 0, 0] = np.float32(rng.uniform(10, 100))
+        vg[pg, 0, 1] = np.float32(-(p[1] * b) / (p[0] * a) * np.float64(vg[pg, 0, 0]))
+        rows[s] = [keys[:, None], (v[pg, 0, :2, :dim].astype(np.float64) / vg[pg, 0, :2].astype(np.float64)[:, None])[:, None]]
+        rows[s][0] = rows[s][0][..., :dim]
+    for t, h in ((C.k, k), (C.v, v), (C.kg, kg), (C.vg, vg)):
+        t.copy_(torch.from_numpy(h))
+    O = attend(C, q, [2] * n, scale)
+    for s in range(n):
+        want, _, spread, big = B.attend(q[s], *rows[s], scale)
+        assert (np.abs(want[:, 0]) < 2.0 ** -20 * spread[:, 0]).all()                    # they cancel
+        tol = HALF * np.abs(want) + (2 * (dim + 8) * 2.0 ** -23 * big[:, None] + W) * spread
+        assert (np.abs(O[s] - want) <= tol).all(), (s, float((np.abs(O[s] - want) / tol).max()))
