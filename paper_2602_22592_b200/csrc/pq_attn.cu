@@ -21,8 +21,9 @@
 //     fp16, where codes are exact and cost least to make: queries are scaled by a power of two per row (exact down to 2^-32 of the row's
 //     largest: bf16 has fewer bits), and the weights, 2^14 at most, enter as the sum of two fp16 numbers, 2^-22 relative down to 2^-17 of
 //     the largest and 2^-39 of the largest below that.  (One number, 2^-11, shows where values cancel.)  gamma_k
-//     scales the scores; the weights are taken with their 1 / gamma_v inside the exponent, exp2(s - log2 gamma_v - m), m the
-//     maximum of that, so that they stay in range, and the sum of weights puts gamma_v back.
+//     scales the scores; the weights of the second product are w / gamma_v, w = exp2(s - m) with m the maximum of s - log2 gamma_v less 14,
+//     so that they stay in range.  m is an offset and nothing else (an approximate logarithm will do), and what is summed up is w itself:
+//     gammas from 2^-121 to 2^24, rows of the largest numbers and rows of zeros, may lie beside one another.
 // Measured (us, GB/s of the cache): sixty-four ragged sequences of up to 4096 positions, eight heads of 128 with four query heads each, bf16
 // 111, 6050; 131072 positions of one sequence, the same heads, int8 58.7, 4720; sixteen of up to 2048, sixteen heads 35, 4910; sixteen of
 // up to 2048, thirty-two heads of 100, int8 41, 3400; one of 200, sixteen heads 7.6.  While the tiles stream they come at the rate of
@@ -107,6 +108,8 @@ __device__ __forceinline__ bool count_last(unsigned long long* word, int of) {
 __device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p) : "memory"); }
 __device__ __forceinline__ float attn_exp2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float attn_log2(float x) { float y; asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+// Factors are taken as the square of this: a sum of weights times it twice survives where its square is below fp32's range
+__device__ __forceinline__ float attn_half(float d) { return attn_exp2(0.5f * d); }
 __device__ __forceinline__ float attn_rcp(float x) { float y; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ void ldmatrix4(uint32_t at, uint32_t (&v)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(at) : "memory");
@@ -214,7 +217,11 @@ __device__ __forceinline__ void attn_store(const AttnArgs& a, long long qrow, in
   *reinterpret_cast<uint2*>(a.O + qrow * a.c.dim + dim) = make_uint2(pack_bf16x2(v0 * inv, v1 * inv), pack_bf16x2(v2 * inv, v3 * inv));
 }
 __device__ __forceinline__ float attn_inv(float l) { return l == 0.f ? 0.f : 1.f / l; }      // no weight: zeros
-__device__ __forceinline__ float attn_lse(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2; }
+__device__ __forceinline__ float attn_lse(float m, float l) {      // m and the exponent of l may be large and cancel
+  int e;
+  const float f = frexpf(l, &e);
+  return l == 0.f ? -INFINITY : ((m + (float)e) + log2f(f)) * kLn2;
+}
 
 template <int DP, int NT, bool I8>
 __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_decode(const __grid_constant__ AttnArgs a) {
@@ -485,7 +492,7 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
           sc[nt][1] = __shfl_sync(0xffffffffu, down, 8 * t + 4);
         }
       }
-      // m: maximum of the scores so far, mu: what is taken off them (0 while there is no weight: every score is -infinity)
+      // m: maximum so far of the scores (int8: less log2 gamma_v), mu: what is taken off them (0 while there is no weight: every score is -infinity)
       float o[NT][DP / 16][4] = {}, m[NT][2], mu[NT][2] = {}, l[NT][2] = {};
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) m[nt][0] = m[nt][1] = -INFINITY;
@@ -514,17 +521,20 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
             for (int nt = 0; nt < NT; ++nt) mma_bf16(j & 1 ? s2[nt] : s[nt], w[0], w[1], w[2], w[3], qf[nt][j][0], qf[nt][j][1]);
           }
         }
-        float gv[2] = {1.f, 1.f};
+        float rv[2], lg[2];                                     // int8: 1 / gamma_v, about log2 gamma_v
         if constexpr (I8) {
           const float* gm = reinterpret_cast<const float*>(smem + F::kGammaAt + warp * (F::kStages * F::kGammaBytes) + stage * F::kGammaBytes);
           const float rk[2] = {attn_rcp(gm[g]), attn_rcp(gm[g + 8])};
-          gv[0] = gm[16 + g];
-          gv[1] = gm[24 + g];
-          const float lg[2] = {attn_log2(gv[0]), attn_log2(gv[1])};
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const float gv = gm[16 + 8 * r + g];
+            rv[r] = attn_rcp(gv);
+            lg[r] = gv == gv ? attn_log2(gv) : 0.f;             // a row that is not a number moves no offset
+          }
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[nt][i] = (s[nt][i] + s2[nt][i]) * (rk[i >> 1] * sc[nt][i & 1]) - lg[i >> 1];
+            for (int i = 0; i < 4; ++i) s[nt][i] = (s[nt][i] + s2[nt][i]) * (rk[i >> 1] * sc[nt][i & 1]);
         } else {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
@@ -536,7 +546,7 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             if (g + 8 * (i >> 1) >= valid) {
-              gv[i >> 1] = 0.f;
+              if constexpr (I8) rv[i >> 1] = lg[i >> 1] = 0.f;
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) s[nt][i] = -INFINITY;
             }
@@ -547,7 +557,7 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            float v = fmaxf(s[nt][c], s[nt][c + 2]);
+            float v = I8 ? fmaxf(s[nt][c] - lg[0], s[nt][c + 2] - lg[1]) : fmaxf(s[nt][c], s[nt][c + 2]);
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
             top[nt][c] = v;
@@ -559,10 +569,10 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
               if (!(top[nt][c] > m[nt][c])) continue;
-              const float f = attn_exp2(m[nt][c] - top[nt][c]);
+              const float h = attn_half(m[nt][c] - top[nt][c]), f = h * h;
               m[nt][c] = top[nt][c];
               mu[nt][c] = I8 ? top[nt][c] - kWeightTop : top[nt][c];
-              l[nt][c] *= f;
+              l[nt][c] = l[nt][c] * h * h;
 #pragma unroll
               for (int i = 0; i < DP / 16; ++i) { o[nt][i][c] *= f; o[nt][i][c + 2] *= f; }
             }
@@ -574,7 +584,8 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             p[i] = attn_exp2(s[nt][i] - mu[nt][i & 1]);
-            l[nt][i & 1] = I8 ? fmaf(p[i], gv[i >> 1], l[nt][i & 1]) : l[nt][i & 1] + p[i];
+            l[nt][i & 1] += p[i];
+            if constexpr (I8) p[i] *= rv[i >> 1];
           }
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
@@ -703,8 +714,8 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
     float top = ml.x, l;
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    const float f = attn_exp2(ml.x - (top == -INFINITY ? 0.f : top));
-    l = ml.y * f;
+    const float h = attn_half(ml.x - (top == -INFINITY ? 0.f : top)), f = h * h;
+    l = ml.y * h * h;
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
     if (in) piece_ml[lane][q].x = f;
@@ -793,8 +804,8 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
         float4 acc = make_float4(0, 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < kFewPieces; ++i) {
-          const float f = attn_exp2(ml[i].x - off);
-          l += ml[i].y * f;
+          const float h = attn_half(ml[i].x - off), f = h * h;
+          l += ml[i].y * h * h;
           acc.x += v[i].x * f; acc.y += v[i].y * f; acc.z += v[i].z * f; acc.w += v[i].w * f;
         }
         out(q, dim, acc, top, l);
@@ -813,9 +824,9 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
       const float off = top == -INFINITY ? 0.f : top;
       for (int i = lane; i < np; i += 32) {
         const float2 ml = __ldcg(&a.cta_ml[slot_of(i) * kQ + q]);
-        const float f = attn_exp2(ml.x - off);
-        fac[i * kQ + q] = f;
-        l += ml.y * f;
+        const float h = attn_half(ml.x - off);
+        fac[i * kQ + q] = h * h;
+        l += ml.y * h * h;
       }
 #pragma unroll
       for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);

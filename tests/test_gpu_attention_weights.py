@@ -58,3 +58,41 @@ def test_int8_weights_where_values_cancel(dim, group):
         assert (np.abs(want[:, 0]) < 2.0 ** -20 * spread[:, 0]).all()                    # they cancel
         tol = HALF * np.abs(want) + (2 * (dim + 8) * 2.0 ** -23 * big[:, None] + W) * spread
         assert (np.abs(O[s] - want) <= tol).all(), (s, float((np.abs(O[s] - want) / tol).max()))
+
+
+@pytest.mark.parametrize("length,at", [(3, 1), (40, 39), (40, 0), (700, 333), (9000, 8999), (9000, 0)])
+def test_int8_rows_of_zeros_beside_very_large_ones(length, at):
+    # equal scores; one row of 2^126 (gamma 2^-119), the others zeros (gamma 2^23): every position counts in the weights' sum
+    rng = np.random.default_rng(42)
+    dim = 64
+    C = Cache(rng, [length], 1, dim, 16, True)
+    rows = C.fill(rng, [length])
+    x = np.zeros((length, 1, dim))
+    x[at] = 2.0 ** 126
+    codes, gamma = B.quantise(x)
+    pos = np.arange(length)
+    pg, o = (torch.from_numpy(a).to(DEV).long() for a in (C.table_host[0, pos // 16], pos % 16))
+    C.v[pg, 0, o, :dim], C.vg[pg, 0, o] = torch.from_numpy(codes[:, 0]).to(DEV), torch.from_numpy(gamma[:, 0]).to(DEV)
+    q, lse = np.zeros((1, 1, dim)), torch.empty((1, 1), device=DEV)
+    O = attend(C, q, [length], 0.125, lse)
+    v = codes.astype(np.float64) / gamma.astype(np.float64)[..., None]
+    want, wl, spread, _ = B.attend(q[0], rows[0][0], v, 0.125)
+    assert (np.abs(O[0] - want) <= HALF * np.abs(want) + (W + length * 2.0 ** -24) * spread).all(), (O[0, 0, 0], want[0, 0])
+    assert abs(float(lse[0, 0]) - wl[0]) <= (length + 8) * 2.0 ** -24 + 2.0 ** -22 * abs(wl[0])
+
+
+def test_the_sum_of_weights_knows_nothing_of_the_values():
+    # int8 rows of values that are not numbers: NaN in the outputs, the log of the weights' sum as ever
+    rng = np.random.default_rng(45)
+    lens = [40, 17, 900]
+    C = Cache(rng, lens, 1, 64, 16, True)
+    rows = C.fill(rng, lens)
+    C.vg[int(C.table_host[0, 1]), 0, 3] = float("nan")
+    C.vg[int(C.table_host[1, 0])] = C.vg[int(C.table_host[1, 1]), :, 0] = float("nan")
+    C.vg[int(C.table_host[2, 30]), 0] = float("nan")
+    q, lse = B.bf16(rng.standard_normal((3, 2, 64))), torch.empty((3, 2), device=DEV)
+    O = attend(C, q, lens, 0.125, lse)
+    assert np.isnan(O).all()
+    for s in range(3):
+        _, wl, _, big = B.attend(q[s], *rows[s], 0.125)
+        assert (np.abs(f64(lse)[s] - wl) <= 72 * 2.0 ** -23 * big + (lens[s] + 8) * 2.0 ** -24 + 2.0 ** -22 * np.abs(wl)).all()
