@@ -16,8 +16,8 @@
 //     nine to sixteen).  tcgen05 has no shape for eight columns by sixteen rows that would not idle.  O^T = V^T P^T with V^T by
 //     transposed ldmatrix.  Of int8 rows a 16-bit element is two codes, neighbours in a row: the contraction index of K and the
 //     rows of V^T are permuted accordingly, queries and outputs with them.
-//   * Types of the products.  A bf16 cache multiplies in bf16, and the weights enter the second product as the sum of two bf16
-//     numbers (2^-16 relative at most): a single rounding of them would be as large as the output's own.  An int8 cache multiplies in
+//   * Types of the products.  A bf16 cache multiplies in bf16, and the weights enter the second product as the sum of three bf16
+//     numbers, eight bits each of the 24 that a weight has, cut off and not rounded: the sum is the weight, and no part has another sign.  An int8 cache multiplies in
 //     fp16, where codes are exact and cost least to make: queries are scaled by a power of two per row (exact down to 2^-32 of the row's
 //     largest: bf16 has fewer bits), and the weights, 2^14 at most, enter as the sum of two fp16 numbers, 2^-22 relative down to 2^-17 of
 //     the largest and 2^-39 of the largest below that.  (One number, 2^-11, shows where values cancel.)  gamma_k
@@ -135,6 +135,9 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
+// The leading eight bits of a number, as a number and, of two, as a pair of bf16
+__device__ __forceinline__ float bf16_part(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+__device__ __forceinline__ uint32_t bf16_parts(float lo, float hi) { return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632); }
 constexpr float kWeightTop = 14.f;        // int8 caches: the largest weight is 2^14, so that small ones keep their bits in fp16
 
 // Division by a number that the host knows, of 0 <= n < 2^31: multiply and shift (Granlund and Montgomery's round-up method)
@@ -577,7 +580,7 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
               for (int i = 0; i < DP / 16; ++i) { o[nt][i][c] *= f; o[nt][i][c + 2] *= f; }
             }
         }
-        uint32_t ph[NT][2], pl[NT][2];
+        uint32_t ph[NT][2], pl[NT][2], pm[I8 ? 1 : NT][2];      // the parts of the weights, largest first
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float p[4];
@@ -595,9 +598,11 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
               ph[nt][h] = transpose8x8(hi);
               pl[nt][h] = transpose8x8(pack_f16x2(p[2 * h] - back.x, p[2 * h + 1] - back.y));
             } else {
-              const uint32_t hi = pack_bf16x2(p[2 * h], p[2 * h + 1]);
-              ph[nt][h] = transpose8x8(hi);
-              pl[nt][h] = transpose8x8(pack_bf16x2(p[2 * h] - bf16lo(hi), p[2 * h + 1] - bf16hi(hi)));
+              const float x = p[2 * h], y = p[2 * h + 1];
+              const float x1 = x - bf16_part(x), y1 = y - bf16_part(y), x2 = x1 - bf16_part(x1), y2 = y1 - bf16_part(y1);
+              ph[nt][h] = transpose8x8(bf16_parts(x, y));
+              pl[nt][h] = transpose8x8(bf16_parts(x1, y1));
+              pm[I8 ? 0 : nt][h] = transpose8x8(bf16_parts(x2, y2));
             }
           }
         }
@@ -621,6 +626,7 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
             for (int nt = 0; nt < NT; ++nt) {
               mma_bf16(o[nt][j], w[0], w[1], w[2], w[3], ph[nt][0], ph[nt][1]);
               mma_bf16(o[nt][j], w[0], w[1], w[2], w[3], pl[nt][0], pl[nt][1]);
+              mma_bf16(o[nt][j], w[0], w[1], w[2], w[3], pm[I8 ? 0 : nt][0], pm[I8 ? 0 : nt][1]);
             }
           }
         }

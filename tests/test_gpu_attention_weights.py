@@ -96,3 +96,53 @@ def test_the_sum_of_weights_knows_nothing_of_the_values():
     for s in range(3):
         _, wl, _, big = B.attend(q[s], *rows[s], 0.125)
         assert (np.abs(f64(lse)[s] - wl) <= 72 * 2.0 ** -23 * big + (lens[s] + 8) * 2.0 ** -24 + 2.0 ** -22 * np.abs(wl)).all()
+
+
+def two_bf16_error(p):
+    """What p loses as the sum of two bf16 numbers, each rounded to nearest, relative to p."""
+    hi = B.bf16(p)
+    return (p - hi - B.bf16(p - hi)) / p
+
+
+@pytest.mark.parametrize("dim,group", [(8, 1), (64, 12), (128, 1), (256, 3)])
+def test_bf16_weights_where_values_cancel(dim, group):
+    # three positions: one takes the maximum and has no value; the weights of the others are such that two bf16 numbers miss one by
+    # +2^-17.x and the other by -2^-17.x, and their values cancel to 2^-12.  The score is one product, 2^k0 after scale = ln 2: its fp32
+    # roundings (of scale log2 e, of the product, of the difference) are 2^-24 of at most 1 each
+    rng = np.random.default_rng(43)
+    scale = float(np.float32(np.log(2)))
+    k0 = -(128 + np.arange(128)) / 256.0                                                   # bf16 numbers in (-1, -1/2]
+    k0 = np.concatenate([k0, k0 / 2])
+    e = two_bf16_error(np.exp(scale * k0).astype(np.float32).astype(np.float64)) * 2.0 ** 17
+    up, down = k0[(e > 0.55) & (e < 0.97)], k0[(e < -0.55) & (e > -0.97)]
+    assert len(up) and len(down)
+    sets = []
+    for ku in up:
+        for kd in down:
+            pu, pd = np.exp(scale * ku), np.exp(scale * kd)
+            a = np.arange(128, 256)
+            b = np.rint(a * pu / pd)
+            off = np.where((b >= 128) & (b < 256), np.abs(a * pu - b * pd) / (a * pu), 1)
+            if off.min() < 2.0 ** -13:
+                sets.append((ku, kd, a[off.argmin()], b[off.argmin()]))
+    assert len(sets) >= 3
+    n = len(sets)
+    C = Cache(rng, [3] * n, 1, dim, 16, False)
+    C.fill(rng, [3] * n)
+    q = np.zeros((n, group, dim))
+    q[:, :, 0] = 1
+    rows = []
+    for s, (ku, kd, a, b) in enumerate(sets):
+        k, v = np.zeros((3, 1, dim)), np.zeros((3, 1, dim))
+        k[:, 0, 0] = [0, ku, kd]
+        v[1, 0], v[2, 0] = a, -b
+        pg = int(C.table_host[s, 0])
+        C.k[pg, 0, :3, :dim], C.v[pg, 0, :3, :dim] = bf(k[:, 0]), bf(v[:, 0])
+        rows.append((k, v))
+    O = attend(C, q, [3] * n, scale)
+    for s in range(n):
+        want, _, spread, _ = B.attend(q[s], *rows[s], scale)
+        # weights: exp2 2^-22, three roundings of the score 3 2^-24 ln 2; the sum: 4 terms cut at 2^-23 of the largest, half of spread.  The
+        # sum that divides moves an output of 2^-12 of spread by nothing that counts
+        tol = HALF * np.abs(want) + (2.0 ** -22 + 3 * 2.0 ** -24 + 4 * 2.0 ** -24) * spread
+        assert (np.abs(O[s] - want) <= tol).all(), (s, float((np.abs(O[s] - want) / tol).max()))
