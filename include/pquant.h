@@ -407,11 +407,12 @@ int pq_kv_read(const pq_kv_cache* c, int tokens, const int32_t* seq, const int32
 
 /* Attention of one token per sequence of the page table over what that sequence keeps:
  *     O[s,h] = sum_j w_j V_j / sum_j w_j,   w_j = exp(scale (Q[s,h] . K_j)),   j < lens[s],
- * K_j, V_j of cache head h / (q_heads / heads).  Scores and sums in fp32; a weight enters the second product whole (bf16 cache);
- * of an int8 cache w_j / gamma_j to 2^-22 of itself or 2^-39 of the sequence's largest; one rounding to bf16.  A sequence of
- * length 0 (and a row without any weight) gives zeros; one of negative length is padding, its row is left as it is.  What lies
- * behind a sequence's length is not read.  A NaN or an infinity within it makes the outputs that it reaches NaN; a score of
- * -infinity is a weight of zero.
+ * K_j, V_j of cache head h / (q_heads / heads).  Scores and sums in fp32; a weight enters the second product whole (bf16 cache,
+ * to 2^-29); of an int8 cache w_j / gamma_j to 2^-22 of itself or 2^-39 of the sequence's largest; one rounding to bf16.  A sequence
+ * of length 0 (and a row without any weight) gives zeros; one of negative length is padding, its row is left as it is.  What lies
+ * behind a sequence's length is not read.  Within it a NaN makes the outputs that it reaches NaN; a score of -infinity is a weight of
+ * zero, one of +infinity makes NaN; an infinity in V gives that infinity, or NaN where it meets the other one or where its weight is
+ * below 2^-80 of the sequence's largest.
  *   Q: rows of q_heads x head_dim bf16, q_stride values apart (0 = dense; a multiple of 4); q_heads a multiple of heads;
  *   lens [num_seqs] int32, at most max_pages * page_size;  scale finite;
  *   O [num_seqs][q_heads][head_dim] bf16;  lse [num_seqs][q_heads] fp32 = log sum_j w_j (-infinity for none), or NULL;

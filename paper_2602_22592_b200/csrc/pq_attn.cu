@@ -17,7 +17,8 @@
 //     transposed ldmatrix.  Of int8 rows a 16-bit element is two codes, neighbours in a row: the contraction index of K and the
 //     rows of V^T are permuted accordingly, queries and outputs with them.
 //   * Types of the products.  A bf16 cache multiplies in bf16, and the weights enter the second product as the sum of three bf16
-//     numbers, eight bits each of the 24 that a weight has, cut off and not rounded: the sum is the weight, and no part has another sign.  An int8 cache multiplies in
+//     numbers, eight bits each of the 24 that a weight has, cut off and not rounded, and 2^-30 of the weight on top: no part is negative or zero (unless
+//     the weight is below 2^-80), so that an infinity among the values stays that infinity.  An int8 cache multiplies in
 //     fp16, where codes are exact and cost least to make: queries are scaled by a power of two per row (exact down to 2^-32 of the row's
 //     largest: bf16 has fewer bits), and the weights, 2^14 at most, enter as the sum of two fp16 numbers, 2^-22 relative down to 2^-17 of
 //     the largest and 2^-39 of the largest below that.  (One number, 2^-11, shows where values cancel.)  gamma_k
@@ -599,7 +600,8 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
               pl[nt][h] = transpose8x8(pack_f16x2(p[2 * h] - back.x, p[2 * h + 1] - back.y));
             } else {
               const float x = p[2 * h], y = p[2 * h + 1];
-              const float x1 = x - bf16_part(x), y1 = y - bf16_part(y), x2 = x1 - bf16_part(x1), y2 = y1 - bf16_part(y1);
+              const float x1 = fmaf(x, 0x1p-30f, x - bf16_part(x)), x2 = fmaf(x, 0x1p-40f, x1 - bf16_part(x1));
+              const float y1 = fmaf(y, 0x1p-30f, y - bf16_part(y)), y2 = fmaf(y, 0x1p-40f, y1 - bf16_part(y1));
               ph[nt][h] = transpose8x8(bf16_parts(x, y));
               pl[nt][h] = transpose8x8(bf16_parts(x1, y1));
               pm[I8 ? 0 : nt][h] = transpose8x8(bf16_parts(x2, y2));

@@ -146,3 +146,30 @@ def test_bf16_weights_where_values_cancel(dim, group):
         # sum that divides moves an output of 2^-12 of spread by nothing that counts
         tol = HALF * np.abs(want) + (2.0 ** -22 + 3 * 2.0 ** -24 + 4 * 2.0 ** -24) * spread
         assert (np.abs(O[s] - want) <= tol).all(), (s, float((np.abs(O[s] - want) / tol).max()))
+
+
+@pytest.mark.parametrize("dim,group,length", [(64, 1, 1), (64, 12, 40), (128, 1, 700), (128, 12, 5000), (100, 2, 37), (256, 3, 90)])
+def test_an_infinity_among_the_values(dim, group, length):
+    # in one value of some positions: that infinity in the outputs it reaches, NaN where both signs meet, the others as ever
+    rng = np.random.default_rng(44)
+    C = Cache(rng, [length], 1, dim, 16, False)
+    (k, v), = C.fill(rng, [length])
+    q = B.bf16(rng.standard_normal((1, group, dim)))
+    scale = dim ** -0.5
+    where = {0: [0], 3: [length - 1], 9: list(range(length)), 20: [length // 2, 0], 31: [length // 3]}
+    for d, at in where.items():
+        v[at, 0, d] = -np.inf if d in (3, 31) else np.inf
+    if length > 1:
+        v[0, 0, 40], v[length - 1, 0, 40] = np.inf, -np.inf
+    pos = np.arange(length)
+    pg, o = (torch.from_numpy(a).to(DEV).long() for a in (C.table_host[0, pos // 16], pos % 16))
+    C.v[pg, 0, o, :dim] = bf(v[:, 0])
+    O = attend(C, q, [length], scale)[0]
+    with np.errstate(invalid="ignore"):
+        want = B.attend(q[0], k, v, scale)[0]
+    assert np.array_equal(np.isnan(want[0]), (np.arange(dim) == 40) & (length > 1)) and np.isposinf(want[:, 9]).all()
+    special = ~np.isfinite(want)
+    assert np.array_equal(O[special], want[special], equal_nan=True), O[special]
+    want, _, spread, big = B.attend(q[0], k, np.where(np.isfinite(v), v, 0), scale)
+    tol = HALF * np.abs(want) + (2 * (dim + 8) * 2.0 ** -23 * big[:, None] + 2.0 ** -16 + length * 2.0 ** -24) * spread + 1e-30
+    assert (np.abs(O - want) <= tol)[~special].all()
