@@ -287,12 +287,23 @@ class PQDecoder:
         return t
 
 
+class _ServedLinear:
+    """A linear's weights as a server keeps them: packed once, every tensor its own."""
+
+    def __init__(self, lin: PQLinearModule):
+        self.K, self.N, self.r, self.E = lin.K, lin.N, lin.r, lin.E
+        self.w_bits, self.w_s8, self.w_scales = (torch.empty_like(t) for t in (lin.w_bits, lin.w_s8, lin.w_scales))
+        pqb.pq_pack_weights(lin.desc, lin.W, self.w_bits, self.w_s8, self.w_scales, lin.ws.pack)
+        self.A, self.B, self.Wr, self.alpha, self.beta = (None if t is None else t.clone() for t in (lin.A, lin.B, lin.Wr, lin.alpha, lin.beta))
+
+
 class PQServer:
     """Serves a PQDecoder's weights to `n` sequences (16 at most: the decode path's tokens): `prompt` takes their first tokens, or more of
     them later, `step` one new token each; both return the logits of every sequence's last token [n, vocab].
 
     The cache has room for `positions` tokens a sequence in pages of `page_size`, handed out as sequences grow; lengths live on the
-    host (a program that admits and frees sequences does so there) and on the device.  Weights are packed when the server is made."""
+    host (a program that admits and frees sequences does so there) and on the device.  Weights are packed and every other parameter is
+    copied when the server is made: what becomes of the model afterwards does not reach it."""
 
     def __init__(self, model: PQDecoder, n, positions, page_size=64, int8_cache=False):
         assert 1 <= n <= 16
@@ -314,9 +325,10 @@ class PQServer:
         self.seq = torch.arange(n, dtype=torch.int32, device=dev)
         self.desc = pqb.make_norm_desc(n, model.hidden, NORM_EPS)
         self.capture = None       # set to a list by tests: receives a dict for every layer of the next call
-        for lin in model.linears():
-            pqb.pq_pack_weights(lin.desc, lin.W, lin.w_bits, lin.w_s8, lin.w_scales, model.ws.pack)
-        self.items = [{names: self._items(blk, names) for names in (("q", "k", "v"), ("o",), ("gate", "up"), ("down",))} for blk in model.blocks]
+        own = lambda t: t.detach().clone()
+        self.blocks = [{name: own(p) if name.startswith("norm") else _ServedLinear(p) for name, p in blk.items()} for blk in model.blocks]
+        self.embed, self.head, self.norm_f = own(model.embed), own(model.head), own(model.norm_f)
+        self.items = [{names: self._items(blk, names) for names in (("q", "k", "v"), ("o",), ("gate", "up"), ("down",))} for blk in self.blocks]
 
     def _items(self, blk, names):
         """Decode descriptors of linears that read the same tokens, with their inputs, outputs and workspaces."""
@@ -359,23 +371,23 @@ class PQServer:
         self._grow([1] * n)
         lens = torch.tensor(self.held, dtype=torch.int32, device=self.dev)
         pos = lens - 1
-        x = m.embed.detach()[ids]
+        x = self.embed[ids]
         h, q_rot, a = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
-        pqb.pq_block_norm_forward(self.desc, x, None, None, None, m.blocks[0]["norm1"].detach(), None, h)
-        for i, blk in enumerate(m.blocks):
+        pqb.pq_block_norm_forward(self.desc, x, None, None, None, self.blocks[0]["norm1"], None, h)
+        for i, blk in enumerate(self.blocks):
             q, k, v = self._decode(i, ("q", "k", "v"), h)
             pqb.pq_kv_append(self.caches[i], self.seq, pos, k, v, self.cos, self.sin, q, q_rot)
             pqb.pq_attn_decode(self.caches[i], q_rot, lens, m.head_dim ** -0.5, a, None, self.attn_ws)
             if self.capture is not None:
                 self.capture.append(dict(q=q.clone(), k=k.clone(), v=v.clone(), q_rot=q_rot.clone(), a=a.clone(), lens=lens.clone(), x=x.clone()))
             y, = self._decode(i, ("o",), a)
-            pqb.pq_block_norm_forward(self.desc, x, y, None, None, blk["norm2"].detach(), x, h)
+            pqb.pq_block_norm_forward(self.desc, x, y, None, None, blk["norm2"], x, h)
             if self.capture is not None:
                 self.capture[-1].update(o=y.clone(), x_out=x.clone(), h=h.clone())
             gate, up = self._decode(i, ("gate", "up"), h)
             y, = self._decode(i, ("down",), F.silu(gate) * up)
-            pqb.pq_block_norm_forward(self.desc, x, y, None, None, (m.blocks[i + 1]["norm1"] if i + 1 < m.layers else m.norm_f).detach(), x, h)
-        return h @ m.head.detach().t()
+            pqb.pq_block_norm_forward(self.desc, x, y, None, None, self.blocks[i + 1]["norm1"] if i + 1 < m.layers else self.norm_f, x, h)
+        return h @ self.head.t()
 
     def prompt(self, ids, lengths):
         """lengths[s] further tokens of every sequence (host integers, at least 1), ids [n, max(lengths)]; what lies behind a sequence's own
@@ -396,9 +408,9 @@ class PQServer:
         all_seq = torch.arange(n, dtype=torch.int32, device=dev).repeat_interleave(most)
         mask = all_at[:, None, :] <= (begin + at)[:, :, None]                                  # [n, S, most]
         desc = pqb.make_norm_desc(T, m.hidden, NORM_EPS)
-        x = m.embed.detach()[ids].reshape(T, m.hidden)
+        x = self.embed[ids].reshape(T, m.hidden)
         h, q_rot = torch.empty_like(x), torch.empty_like(x)
-        pqb.pq_block_norm_forward(desc, x, None, None, None, m.blocks[0]["norm1"].detach(), None, h)
+        pqb.pq_block_norm_forward(desc, x, None, None, None, self.blocks[0]["norm1"], None, h)
 
         def linear(lin, x):
             d = pqb.make_desc(T, lin.K, lin.N, lin.r, lin.E)
@@ -407,7 +419,7 @@ class PQServer:
             pqb.pq_linear_forward(d, x, lin.w_bits, lin.w_s8, lin.w_scales, lin.A, lin.B, lin.Wr, lin.alpha, lin.beta, y, None, ws)
             return y
 
-        for i, blk in enumerate(m.blocks):
+        for i, blk in enumerate(self.blocks):
             q, k, v = (linear(blk[name], h) for name in "qkv")
             q_rot.zero_()                                       # rows of padding are left as they are
             pqb.pq_kv_append(self.caches[i], seq, pos, k, v, self.cos, self.sin, q, q_rot)
@@ -416,11 +428,11 @@ class PQServer:
             heads = lambda t, rows: t.view(n, rows, H, D).transpose(1, 2)
             a = F.scaled_dot_product_attention(heads(q_rot, S), heads(ks, most), heads(vs, most), attn_mask=mask[:, None])
             y = linear(blk["o"], a.transpose(1, 2).reshape(T, m.hidden))
-            pqb.pq_block_norm_forward(desc, x, y, None, None, blk["norm2"].detach(), x, h)
+            pqb.pq_block_norm_forward(desc, x, y, None, None, blk["norm2"], x, h)
             y = linear(blk["down"], F.silu(linear(blk["gate"], h)) * linear(blk["up"], h))
-            pqb.pq_block_norm_forward(desc, x, y, None, None, (m.blocks[i + 1]["norm1"] if i + 1 < m.layers else m.norm_f).detach(), x, h)
+            pqb.pq_block_norm_forward(desc, x, y, None, None, self.blocks[i + 1]["norm1"] if i + 1 < m.layers else self.norm_f, x, h)
         last = torch.arange(n, device=dev) * S + count[:, 0] - 1
-        return h[last] @ m.head.detach().t()
+        return h[last] @ self.head.t()
 
 
 def softmax_entropy_bound(vocab):
