@@ -391,7 +391,7 @@ class PQServer:
 
     def prompt(self, ids, lengths):
         """lengths[s] further tokens of every sequence (host integers, at least 1), ids [n, max(lengths)]; what lies behind a sequence's own
-        tokens is padding.  They attend over what the sequence holds already, and over one another in order."""
+        tokens is padding and may be any number.  They attend over what the sequence holds already, and over one another in order."""
         m, n, S = self.m, self.n, ids.shape[1]
         assert len(lengths) == n and max(lengths) == S and min(lengths) >= 1
         past = list(self.held)
@@ -408,7 +408,7 @@ class PQServer:
         all_seq = torch.arange(n, dtype=torch.int32, device=dev).repeat_interleave(most)
         mask = all_at[:, None, :] <= (begin + at)[:, :, None]                                  # [n, S, most]
         desc = pqb.make_norm_desc(T, m.hidden, NORM_EPS)
-        x = self.embed[ids].reshape(T, m.hidden)
+        x = self.embed[torch.where(at < count, ids.to(dev), 0)].reshape(T, m.hidden)           # a padding id need not be in the vocabulary
         h, q_rot = torch.empty_like(x), torch.empty_like(x)
         pqb.pq_block_norm_forward(desc, x, None, None, None, self.blocks[0]["norm1"], None, h)
 

@@ -41,3 +41,13 @@ def test_a_server_serves_the_weights_it_was_made_with():
     check_status()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     assert not torch.equal(answers(PQServer(m, 2, 40, 16, True))[0], want[0])
+
+
+@pytest.mark.parametrize("pad", [0, -100, 300, -301, 1 << 40])
+def test_what_lies_behind_a_sequences_tokens_names_no_token(pad):
+    m = model(64)
+    lengths = [9, 2, 5]
+    ids = tokens(8, 3, 9)
+    behind = torch.arange(9, device=DEV)[None] >= torch.tensor(lengths, device=DEV)[:, None]
+    want = PQServer(m, 3, 20, 16).prompt(torch.where(behind, 7, ids), lengths)
+    assert torch.equal(PQServer(m, 3, 20, 16).prompt(torch.where(behind, pad, ids), lengths), want)
