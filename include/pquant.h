@@ -414,7 +414,7 @@ int pq_kv_read(const pq_kv_cache* c, int tokens, const int32_t* seq, const int32
  * zero, one of +infinity makes NaN; an infinity in V gives that infinity, or NaN where it meets the other one or where its weight is
  * below 2^-80 of the sequence's largest.
  *   Q: rows of q_heads x head_dim bf16, q_stride values apart (0 = dense; a multiple of 4); q_heads a multiple of heads;
- *   lens [num_seqs] int32, at most max_pages * page_size;  scale finite;
+ *   lens [num_seqs] int32, at most max_pages * page_size;  scale below 2^127 in size;
  *   O [num_seqs][q_heads][head_dim] bf16;  lse [num_seqs][q_heads] fp32 = log sum_j w_j (-infinity for none), or NULL;
  *   ws: pq_attn_workspace_bytes bytes of any content, for one call at a time.
  * Results do not depend on scheduling, but on how the batch is cut into shares: the same sequence in another batch may

@@ -774,7 +774,8 @@ int pq_attn_decode(const pq_kv_cache* c, int q_heads, const uint16_t* Q, int64_t
   if (const int rc = check_kv(c, &kv)) return rc;
   if (!Q || !lens || !O || !ws) return PQ_ERR_NULL;
   if (!q_heads_ok(kv, q_heads) || !row_stride(q_stride, (int64_t)q_heads * kv.dim, &q_stride)) return PQ_ERR_SHAPE;
-  if (!(scale - scale == 0.f)) return PQ_ERR_SHAPE;      // infinite or not a number
+  const float log2_scale = scale * 1.5f;                 // the kernel multiplies by log2 e, which must not overflow either
+  if (!(log2_scale - log2_scale == 0.f)) return PQ_ERR_SHAPE;
   if (misaligned(Q) || misaligned(lens) || misaligned(O) || misaligned(lse) || misaligned(ws)) return PQ_ERR_ALIGN;
   if (ws_bytes < attn_workspace_bytes(kv, q_heads)) return PQ_ERR_WORKSPACE;
   return launch_attn_decode(kv, q_heads, Q, q_stride, lens, scale, O, lse, ws, static_cast<cudaStream_t>(stream)) == cudaSuccess ? PQ_OK : PQ_ERR_CUDA;

@@ -268,3 +268,10 @@ def test_empty_rotary_tables_are_refused(lib, monkeypatch):
     monkeypatch.setattr(lib, "lib", lambda: type("L", (), {"pq_kv_append": staticmethod(lambda *a: 0)}))
     with pytest.raises(lib.PqArgumentError):
         lib.pq_kv_append(cache, at, at, row, row, empty, empty)
+
+
+@pytest.mark.parametrize("scale", [2.5e38, -3.4e38, float("inf"), float("-inf"), float("nan")])
+def test_attention_scales_that_overflow_in_powers_of_two_are_refused(lib, scale):
+    # the kernel takes scale log2(e): infinite for these, and a score of 0 would come out as NaN
+    c = cache(lib)
+    assert lib.lib().pq_attn_decode(ctypes.byref(c), 8, P, 0, P, scale, P, None, P, 1 << 40, None) == lib.PQ_ERR_SHAPE
