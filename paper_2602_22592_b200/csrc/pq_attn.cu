@@ -92,6 +92,12 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// The sum of a tile to that of the tiles before.  A tensor core cuts off what does not fit where it adds to its accumulator: over a thousand tiles
+// that would be 2^-14 of the sum for each part of the weights, always towards zero.  This addition rounds.
+__device__ __forceinline__ void attn_add(float (&o)[4], const float (&sum)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] += sum[i];
+}
 // A word that counts arrivals of one launch: the launch's number above 16 bits, the count below.  Whoever is going to count first makes
 // sure that the word is this launch's (a failed exchange means that another CTA of it did), so that the workspace may hold anything before.
 __device__ __forceinline__ void count_open(unsigned long long* word, unsigned long long call) {
@@ -619,16 +625,20 @@ __global__ void __launch_bounds__(AttnForm<DP, NT, I8>::kWarps * 32, 1) k_attn_d
               const uint32_t a0 = codes_pair<0x4240>(x0), a1 = codes_pair<0x4341>(x0), a2 = codes_pair<0x4240>(x1), a3 = codes_pair<0x4341>(x1);
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) {
-                mma_f16(o[nt][2 * j + h], a0, a1, a2, a3, ph[nt][0], ph[nt][1]);
-                mma_f16(o[nt][2 * j + h], a0, a1, a2, a3, pl[nt][0], pl[nt][1]);
+                float sum[4] = {};
+                mma_f16(sum, a0, a1, a2, a3, pl[nt][0], pl[nt][1]);
+                mma_f16(sum, a0, a1, a2, a3, ph[nt][0], ph[nt][1]);
+                attn_add(o[nt][2 * j + h], sum);
               }
             }
           } else {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-              mma_bf16(o[nt][j], w[0], w[1], w[2], w[3], ph[nt][0], ph[nt][1]);
-              mma_bf16(o[nt][j], w[0], w[1], w[2], w[3], pl[nt][0], pl[nt][1]);
-              mma_bf16(o[nt][j], w[0], w[1], w[2], w[3], pm[I8 ? 0 : nt][0], pm[I8 ? 0 : nt][1]);
+              float sum[4] = {};
+              mma_bf16(sum, w[0], w[1], w[2], w[3], pm[I8 ? 0 : nt][0], pm[I8 ? 0 : nt][1]);
+              mma_bf16(sum, w[0], w[1], w[2], w[3], pl[nt][0], pl[nt][1]);
+              mma_bf16(sum, w[0], w[1], w[2], w[3], ph[nt][0], ph[nt][1]);
+              attn_add(o[nt][j], sum);
             }
           }
         }

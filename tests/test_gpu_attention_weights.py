@@ -173,3 +173,37 @@ def test_an_infinity_among_the_values(dim, group, length):
     want, _, spread, big = B.attend(q[0], k, np.where(np.isfinite(v), v, 0), scale)
     tol = HALF * np.abs(want) + (2 * (dim + 8) * 2.0 ** -23 * big[:, None] + 2.0 ** -16 + length * 2.0 ** -24) * spread + 1e-30
     assert (np.abs(O - want) <= tol)[~special].all()
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("dim,group", [(64, 1), (64, 16), (128, 1), (128, 16), (256, 3)])
+def test_long_sums_lean_to_neither_side(dim, group, int8):
+    # 131072 positions, the same eight pages over and over, values of one sign; enough sequences that a warp has thousands of tiles of one.  An
+    # output's rounding to bf16 is at most 2^-8 either way, a deviation of 2^-8 / sqrt(3): the mean over all outputs stays within six
+    # of its own deviations, and 2^-20 for what a tile's sum (cut off at 2^-23) and a reciprocal (2^-23) may lean by
+    g = torch.Generator(device=DEV)
+    g.manual_seed(46)
+    page, pages, length, n, heads = 128, 8, 131072, 148, 8 if group == 1 else 2
+    k, v = (torch.randn((pages, heads, page, dim), generator=g, device=DEV) for _ in range(2))
+    v = v * 0.3 + 1.5
+    kg = vg = None
+    if int8:
+        kg, vg = 128 / k.abs().amax(-1), 128 / v.abs().amax(-1)
+        k, v = ((x * y[..., None]).round().clamp(-128, 127).to(torch.int8) for x, y in ((k, kg), (v, vg)))
+        rows = [x.double() / y.double()[..., None] for x, y in ((k, kg), (v, vg))]
+    else:
+        k, v = k.to(torch.bfloat16), v.to(torch.bfloat16)
+        rows = [k.double(), v.double()]
+    table = (torch.arange(length // page, device=DEV, dtype=torch.int32) % pages).repeat(n, 1)
+    c = pqb.make_kv_cache(k, v, table, dim, kg, vg)
+    H = heads * group
+    q = torch.randn((n, H * dim), generator=g, device=DEV).to(torch.bfloat16)
+    O = torch.empty_like(q)
+    ws = torch.empty(pqb.pq_attn_workspace_bytes(c, H), dtype=torch.uint8, device=DEV)
+    pqb.pq_attn_decode(c, q, torch.full((n,), length, dtype=torch.int32, device=DEV), dim ** -0.5, O, None, ws)
+    check_status()
+    keys, values = (x.transpose(0, 1).reshape(heads, -1, dim) for x in rows)
+    weight = torch.softmax(torch.einsum("nhgd,hpd->nhgp", q.double().view(n, heads, group, dim), keys) * dim ** -0.5, -1)
+    want = torch.einsum("nhgp,hpd->nhgd", weight, values).reshape(n, -1)
+    lean = float(((O.double() - want) / want).mean())
+    assert abs(lean) <= 6 * HALF / np.sqrt(3 * want.numel()) + 2.0 ** -20, lean
