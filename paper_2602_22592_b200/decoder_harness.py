@@ -306,7 +306,8 @@ class PQServer:
     copied when the server is made: what becomes of the model afterwards does not reach it."""
 
     def __init__(self, model: PQDecoder, n, positions, page_size=64, int8_cache=False):
-        assert 1 <= n <= 16
+        if not 1 <= n <= 16:
+            raise ValueError(f"{n} sequences: the decode path takes 1 to 16")
         self.m, self.n, self.positions = model, n, positions
         dev, H, D, L = model.dev, model.heads, model.head_dim, model.layers
         self.dev = dev
@@ -368,6 +369,8 @@ class PQServer:
     def step(self, ids):
         """One new token of every sequence: ids [n]."""
         m, n = self.m, self.n
+        if ids.shape != (n,):
+            raise ValueError(f"ids has to be [{n}], one token of every sequence")
         self._grow([1] * n)
         lens = torch.tensor(self.held, dtype=torch.int32, device=self.dev)
         pos = lens - 1
@@ -392,8 +395,9 @@ class PQServer:
     def prompt(self, ids, lengths):
         """lengths[s] further tokens of every sequence (host integers, at least 1), ids [n, max(lengths)]; what lies behind a sequence's own
         tokens is padding and may be any number.  They attend over what the sequence holds already, and over one another in order."""
-        m, n, S = self.m, self.n, ids.shape[1]
-        assert len(lengths) == n and max(lengths) == S and min(lengths) >= 1
+        m, n, S = self.m, self.n, ids.shape[-1]
+        if ids.shape != (n, S) or len(lengths) != n or max(lengths) != S or min(lengths) < 1:
+            raise ValueError(f"ids has to be [{n}, longest of lengths], and every sequence has to get a token")
         past = list(self.held)
         self._grow(lengths)
         T, H, D, dev = n * S, m.heads, m.head_dim, self.dev

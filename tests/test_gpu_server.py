@@ -165,3 +165,20 @@ def test_a_prompt_in_pieces_and_by_steps_keeps_what_one_prompt_keeps(int8):
             pair = np.abs(a) + np.abs(np.roll(a, 32, -1)) + np.abs(b)
             tol = 4 * HALF * pair + (np.abs(a).max(-1, keepdims=True) / 128 * 1.01 if int8 else 0)
             assert (np.abs(a - b) <= tol).all() and np.abs(a).max() > 0
+
+
+def test_a_refused_call_changes_nothing():
+    # ids of another shape: refused before the sequences grow, so that the next call's tokens stand where they belong
+    m = model(65)
+    S, other = PQServer(m, 2, 20, 16), PQServer(m, 2, 20, 16)
+    S.prompt(tokens(1, 2, 3), [3, 2])
+    for bad in (lambda: S.step(tokens(2, 3)), lambda: S.step(tokens(2, 2, 1)), lambda: S.prompt(tokens(2, 3, 4), [4, 4]), lambda: S.prompt(tokens(2, 4), [4, 4]),
+                lambda: S.prompt(tokens(2, 2, 4), [4, 3, 1]), lambda: S.prompt(tokens(2, 2, 4), [3, 3]), lambda: S.prompt(tokens(2, 2, 4), [4, 0])):
+        with pytest.raises(ValueError):
+            bad()
+    for n in (0, 17):
+        with pytest.raises(ValueError):
+            PQServer(m, n, 20, 16)
+    assert S.held == [3, 2]
+    other.prompt(tokens(1, 2, 3), [3, 2])
+    assert torch.equal(S.step(tokens(4, 2)), other.step(tokens(4, 2)))
