@@ -1,9 +1,10 @@
 // Attention of one new token per sequence over the paged key-value cache:
 //     o = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale (q . k_j) - m),   m = max_j scale (q . k_j),   j < length of the sequence.
 //
-// A pass reads every cached row once and multiplies it with the group x head_dim query values that share its head: one to
-// sixteen multiplications per byte, far below what the tensor cores need to be the limit, so that the memory is.  What
-// follows from that:
+// A pass reads every cached row and multiplies it with the group x head_dim query values that share its head: one to
+// sixteen multiplications per byte, far below what the tensor cores need to be the limit, so that the memory is.  (Rows are read once for
+// each column block: of sixteen query heads, or of eight above head_dim 128.  More query heads to a cache head than that read them again.)
+// What follows from that:
 //   * A warp works alone while it reads: it walks tiles of sixteen positions, copies them asynchronously in whole lines (a copy of a
 //     warp is 512 neighbouring bytes; 16 bytes here and there in eight rows at once reached 4.5 TB/s, lines reach 5.9) into a ring
 //     of its own, and meets no barrier.  The ring, 200 KB per SM, covers the latency.  Its 16-byte pieces are swizzled, so that
@@ -26,12 +27,13 @@
 //     so that they stay in range.  m is an offset and nothing else (an approximate logarithm will do), and what is summed up is w itself:
 //     gammas from 2^-121 to 2^24, rows of the largest numbers and rows of zeros, may lie beside one another.
 // Measured (us, GB/s of the cache): sixty-four ragged sequences of up to 4096 positions, eight heads of 128 with four query heads each, bf16
-// 111, 6050; 131072 positions of one sequence, the same heads, int8 58.7, 4720; sixteen of up to 2048, sixteen heads 35, 4910; sixteen of
-// up to 2048, thirty-two heads of 100, int8 41, 3400; one of 200, sixteen heads 7.6.  While the tiles stream they come at the rate of
-// the memory; beside that a call has a head of about 4 us (lengths, page ids, first rows: three trips to memory one after another) and a tail
-// of 3 to 5 (warps that end apart, two joins, the count between CTAs).  int8 rows also cost instructions, a third of them conversions: 60 % of
-// the issue slots.  Eight or twelve warps instead of sixteen: heads of 100 47 and 41; addresses carried along, pieces behind head_dim
-// skipped, rows packed densely in the ring: no gain.
+// 112 to 116, 5900; 131072 positions of one sequence, the same heads, int8 62 to 65, 4300; sixteen of up to 2048, sixteen heads 35, 4900;
+// sixteen of up to 2048, thirty-two heads of 100, int8 45, 3100; one of 200, sixteen heads 7.6.  Sixteen of up to 4096, eight heads of 256, bf16, with 8,
+// 16 and 32 query heads each: 100, 143 and 237.  While the tiles stream they come at the rate of the memory; beside that a call has a head
+// of about 4 us (lengths, page ids, first rows: three trips to memory one after another) and a tail of 3 to 5 (warps that end apart, two
+// joins, the count between CTAs).  int8 rows also cost instructions, three in ten of them conversions: 62 % of the issue slots.  Eight or
+// twelve warps instead of sixteen: heads of 100 47 and 41 where sixteen took 41; addresses carried along, pieces behind head_dim skipped,
+// rows packed densely in the ring: no gain.
 #include <cuda_fp16.h>
 
 #include <algorithm>

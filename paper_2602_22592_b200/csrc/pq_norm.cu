@@ -7,6 +7,9 @@
 // Measured at 8192 x 2048 with a norm behind the block and a gate per feature: forward 30 us (134 MB, 4.5 TB/s; a copy of as much 20.5), backward
 // 50 us (201 MB, 4.0 TB/s).  The forward waits at two meetings of a row's warps; the backward issues in 69 % of its slots: 27 fp32 operations a
 // value and as much again to unpack, address and add up.  999 x 3200 without a norm behind the block: 18 us, 5 of them the sums over blocks.
+// Above N = 2048 the backward behind a norm needs more than the 128 registers a thread has (two or four pieces, two rows, three running sums): 70 to 490
+// bytes of it live in local memory for two pieces, 400 to 940 for four, and it shows: 4096 x 3200 with a gate per feature 87 us, without a norm
+// behind the block 32; 1024 x 8640 97 and 28.
 #include <algorithm>
 #include <mutex>
 
